@@ -105,7 +105,9 @@ typedef enum {
   RESQ_OP_LINEAR_FWD_PREPARED = 3,
   RESQ_OP_DIAGNOSTICS = 4,
   RESQ_OP_LINEAR_W16A4 = 5,
-  RESQ_OP_LINEAR_FWD_RMSNORM = 6
+  RESQ_OP_LINEAR_FWD_RMSNORM = 6,
+  RESQ_OP_BLOCK_NORM_BWD = 7,  /* m, d; the other arguments are ignored */
+  RESQ_OP_TOKEN_LOGPROBS = 8   /* m, d = V, n = top_k; the other arguments are ignored */
 } resq_op;
 
 /*
@@ -326,6 +328,101 @@ int resq_linear_w16a4(int format, const uint16_t* X, int64_t m, int64_t d, int64
                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * resq_matvec_w4a16 - resq_linear_w4a16 for the few tokens of a rollout's tail: Y = X Q(W)^T for
+ * m <= 16 rows (RESQ_ERR_UNSUPPORTED beyond), bound by one read of Q(W).
+ * X: m x d bf16, any row stride ldx >= d, 2-byte aligned.  Q(W): K-major codes and scales as for
+ *   resq_linear_w4a16 (codes 16-byte, HiF4 scales 4-byte aligned).  d: a multiple of the block.
+ * Y: m x n, row stride ldy >= n, float32 (y_dtype = RESQ_IN_F32) or bf16 (RESQ_IN_BF16: the
+ *   float32 result rounded once, ties to even).  d = 0 writes zeros.
+ * Products are exact; the sum over d is float32, in an order fixed by the sizes.  Sums may
+ * therefore differ from resq_linear_w4a16's in their last bits.  No workspace.
+ */
+int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64_t ldx,
+                      const uint8_t* qw_codes, const void* qw_scales, int64_t n, void* Y, int y_dtype,
+                      int64_t ldy, void* stream);
+
+/*
+ * Norms before and after a block, with the block's gate, its residual scale and the residual
+ * addition: what stands between the output of one linear and the input of the next.
+ *
+ * resq_block_norm_fwd - per row:
+ *     t  = Y r_post gamma_post     (t = Y when gamma_post is NULL)
+ *     H' = H + alpha g t           rounded once to H's type
+ *     X  = H' r_pre gamma_pre      of the rounded H'; bf16(f32(f32(H' r) gamma))
+ * with r = 1 / sqrt(mean(row^2) + eps), the sum of squares in float64 and the rest as
+ * resq_linear_fwd_prepared_rmsnorm defines it, so that X is the input that entry point forms.
+ * H, H_out : m x d of h_dtype (RESQ_IN_BF16 or RESQ_IN_F32), row strides ldh, ldho.  H_out may be H.
+ * Y        : m x d of y_dtype, row stride ldy (a linear's output).  NULL: X = norm of H only; then
+ *            gamma_pre is required, gamma_post and a gate are errors, and H_out is not written.
+ * gamma_post, gamma_pre : d bf16 values, or NULL (no norm there; without gamma_pre X is not
+ *            written and may be NULL).
+ * gate     : of gate_dtype: one value per channel (RESQ_GATE_CHANNEL, d values), per row
+ *            (RESQ_GATE_TOKEN, m values), or none (RESQ_GATE_NONE, gate ignored).
+ * rstd     : 2 x m float32 outputs, r_post then r_pre (0 for an absent norm), which the backward
+ *            reads; NULL to skip.
+ * Pointers are aligned to their elements; every row stride >= d.  d <= 16384 and m < 2^31
+ * (RESQ_ERR_UNSUPPORTED beyond).  Apart from H_out = H, outputs overlap no input.  No workspace.
+ *
+ * resq_block_norm_bwd - the gradients, given those of X (dX, of dx_dtype: resq_linear_bwd's
+ * float32 dX, or bf16) and of H' (dH_out, of h_dtype; NULL: zero):
+ *     dH (h_dtype), dY (dy_dtype; bf16 is what resq_linear_bwd takes), dgamma_post, dgamma_pre (d
+ *     float32) and dgate (float32: d values per channel, or m per row); each may be NULL.
+ * H is the forward's H_out, and rstd its output.  H and dX are read only with gamma_pre, Y only
+ * where a wanted gradient needs it (dY or dgamma_post with gamma_post, or dgate).  dH may be
+ * dH_out.  Every sum is float32 or wider, in an order fixed by the sizes.
+ * Workspace: resq_workspace_size(RESQ_OP_BLOCK_NORM_BWD, 0, 0, m, d, 0) bytes.
+ */
+enum { RESQ_GATE_NONE = 0, RESQ_GATE_CHANNEL = 1, RESQ_GATE_TOKEN = 2 };
+int resq_block_norm_fwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_t ldh, const void* Y,
+                        int y_dtype, int64_t ldy, const uint16_t* gamma_post, const void* gate,
+                        int gate_dtype, int gate_mode, float alpha, const uint16_t* gamma_pre,
+                        float eps, void* H_out, int64_t ldho, uint16_t* X, int64_t ldx, float* rstd,
+                        void* stream);
+int resq_block_norm_bwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_t ldh, const void* Y,
+                        int y_dtype, int64_t ldy, const uint16_t* gamma_post, const void* gate,
+                        int gate_dtype, int gate_mode, float alpha, const uint16_t* gamma_pre,
+                        const float* rstd, const void* dX, int dx_dtype, int64_t lddx, const void* dH_out,
+                        int64_t lddho, void* dH, int64_t lddh, void* dY, int dy_dtype, int64_t lddy,
+                        float* dgamma_post, float* dgamma_pre, float* dgate, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * resq_token_logprobs - log probabilities of given tokens under a policy's logits (a linear's Y),
+ * with the entropy and the top alternatives.  Per row x of V logits, at a temperature T:
+ *     log p_j = x_j / T - log sum_i exp(x_i / T),   H = -sum_j p_j log p_j
+ * logits  : m x V of dtype (RESQ_IN_F32 or RESQ_IN_BF16), row stride ld >= V, aligned to its
+ *           element.  -inf bans a token (probability 0, no part of H).  1 <= V < 2^31.
+ * targets : m token numbers, or NULL (no logp).  A negative one marks a row without a target (a
+ *           prompt's or padding): its logits are not read, its logp and stats are 0 and it has no
+ *           alternatives.  One past V - 1 gives logp NaN.
+ * temperature : in [2^-64, 2^64].
+ * logp    : m float32, log p of the targets; NULL to skip.
+ * stats   : m x 3 float32: max x, log sum exp((x - max x) / T), H.
+ * top_k   : 0..32 alternatives per row into top_logp (m x top_k float32) and top_index (m x top_k
+ *           int32), by descending logit, equal logits by ascending index; past the last token that
+ *           is not banned: -inf and -1.
+ * A row of -inf alone gives logp -inf, stats (-inf, -inf, 0) and no alternatives; a row with a NaN
+ * or +inf logit gives NaN.
+ * Sums are float32, in an order fixed by the sizes.  Workspace:
+ * resq_workspace_size(RESQ_OP_TOKEN_LOGPROBS, 0, 0, m, V, top_k) bytes.
+ *
+ * resq_token_logprobs_bwd - the gradient of the logits, given those of logp (dlogp, m float32) and
+ * of H (dentropy, m float32), either NULL for zero:
+ *     dlogits_j = (dlogp (delta_jt - p_j) - dentropy p_j (log p_j + H)) / T
+ * in out_dtype (bf16 is what resq_linear_bwd takes as dY), row stride ldd >= V.  stats is the
+ * forward's.  Rows without a target, and rows of -inf alone, get zeros; a target past V - 1 NaN.
+ * dlogits may be logits when the types and strides are equal.  No workspace.
+ */
+int resq_token_logprobs(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld,
+                        const int64_t* targets, double temperature, float* logp, float* stats,
+                        int top_k, float* top_logp, int32_t* top_index, void* workspace,
+                        size_t workspace_bytes, void* stream);
+int resq_token_logprobs_bwd(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld,
+                            const int64_t* targets, double temperature, const float* stats,
+                            const float* dlogp, const float* dentropy, void* dlogits, int out_dtype,
+                            int64_t ldd, void* stream);
+
+/*
  * The GEMM plan a call of these sizes runs (host-side query; nothing is enqueued and no GPU
  * is needed).  The GEMM computes Y[M][N] = sum over K: the forward linear has M = m, N = n,
  * K = d and may split K (split_allowed = 1); the backward's dX GEMM has M = m, N = d, K = n,
@@ -349,12 +446,14 @@ const char* resq_version(void);
  * Kernel timing (diagnostics; off by default).  While enabled, every kernel the library
  * enqueues is timed with two HIP events on the same stream (event objects are host-side
  * handles; no device memory is allocated).  The GEMMs ("gemm", with a K split's reduction),
- * the forward's activation pass ("residual" in the forward entry points) and "diagnostics"
- * carry the events in their kernel dispatches, so the interval is the kernels' execution as a
+ * the forward's activation pass ("residual" in the forward entry points), "diagnostics",
+ * "block_norm", "matvec" and "logprobs" carry the events in their kernel dispatches, so the
+ * interval is the kernels' execution as a
  * kernel trace measures it; the other families record them around the enqueue, which adds
  * the dispatch gap (a few microseconds).  resq_profile_read synchronizes the
  * recorded events and returns, for the kernel family `name` ("residual", "quant_rows",
- * "quant_cols", "pack_hif4", "select", "gemm", "diagnostics", "mixed"), the number of launches and their summed
+ * "quant_cols", "pack_hif4", "select", "gemm", "diagnostics", "mixed", "block_norm", "matvec",
+ * "logprobs"), the number of launches and their summed
  * duration in milliseconds since the last reset.  Returns RESQ_ERR_ARG for an unknown name.
  */
 int resq_profile_enable(int on);

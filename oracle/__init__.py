@@ -16,6 +16,8 @@ Contents
 ``resq``     residual (Eq. 2), the sparsity functions S (Sec. 4.3), the forward of Eq. 1,
              Eq. 3 and Eq. 4, the mixed-precision W4A16 / W16A4 linears of Table 1, the FP4
              backward GEMMs of the training policy, and the overhead cost model of Sec. 5.4.
+``operators``  the operators around the linears: norms before and after a block, the few-token
+             product with 4-bit weights, token log probabilities, with their gradients.
 
 Pins: every function here is checked by ``tests/test_oracle_*.py`` against facts fixed
 outside this package (value sets, exhaustive bf16 sweeps against independent integer
@@ -24,4 +26,4 @@ functions are pinned to the reading written in ``formats``; whether that reading
 external HiF4 specification is not checked (the specification is not available here), so
 the HiF4 *format definition itself* is "parity unpinned" against that specification.
 """
-from . import formats, resq  # noqa: F401
+from . import formats, operators, resq  # noqa: F401

@@ -1,0 +1,119 @@
+"""The operators around the FP4 linears, in float64: norms before and after a block with their
+gradients, the matrix-vector product with 4-bit weights, token log probabilities with theirs.
+
+Plain statements of the definitions in ``include/resq.h`` on NumPy arrays; nothing is rounded
+except where a definition names a stored value (the norm after a residual update is that of the
+stored stream, which the caller passes rounded).
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from . import formats as F
+
+
+def rms_factor(x, eps):
+    x = np.asarray(x, np.float64)
+    return 1.0 / np.sqrt(np.mean(x * x, axis=1) + eps)
+
+
+def block_update(h, y, gamma_post=None, gate=None, alpha=1.0, eps=1e-6):
+    """h + alpha * gate * (RMSNorm(y) * gamma_post), unrounded, and the norm's row factors (or
+    None).  gate broadcasts: d values, or m x 1."""
+    t, r = np.asarray(y, np.float64), None
+    if gamma_post is not None:
+        r = rms_factor(t, eps)
+        t = t * r[:, None] * np.asarray(gamma_post, np.float64)
+    if gate is not None:
+        t = t * np.asarray(gate, np.float64)
+    return np.asarray(h, np.float64) + alpha * t, r
+
+
+def rms_norm(h, gamma, eps=1e-6):
+    """RMSNorm(h) * gamma and the row factors."""
+    r = rms_factor(h, eps)
+    return np.asarray(h, np.float64) * r[:, None] * np.asarray(gamma, np.float64), r
+
+
+def block_norm_bwd(h_out, y, r_post, r_pre, dx, dh_out, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None):
+    """Gradients of h_out = block_update(...) and x = rms_norm(h_out, gamma_pre) with the row
+    factors given: dict of dh, dy, dgamma_post, dgamma_pre, dgate (None where there is none)."""
+    h, y, e = (np.asarray(v, np.float64) for v in (h_out, y, dh_out))
+    out = {"dgamma_post": None, "dgamma_pre": None, "dgate": None}
+    if gamma_pre is not None:
+        dx, g = np.asarray(dx, np.float64), np.asarray(gamma_pre, np.float64)
+        n = h * r_pre[:, None]
+        u = dx * g
+        out["dgamma_pre"] = (dx * n).sum(0)
+        e = e + r_pre[:, None] * (u - n * (u * n).mean(1, keepdims=True))
+    n = y if gamma_post is None else y * r_post[:, None]
+    gp = 1.0 if gamma_post is None else np.asarray(gamma_post, np.float64)
+    gt = 1.0 if gate is None else np.asarray(gate, np.float64)
+    if gate is not None:
+        full = alpha * e * n * gp
+        out["dgate"] = full.sum(1, keepdims=True) if np.ndim(gt) == 2 else full.sum(0)
+    dt = alpha * gt * e
+    dy = dt * np.ones_like(y)
+    if gamma_post is not None:
+        out["dgamma_post"] = (dt * n).sum(0)
+        v = dt * gp
+        dy = r_post[:, None] * (v - n * (v * n).mean(1, keepdims=True))
+    return {"dh": e, "dy": dy, **out}
+
+
+def matvec(fmt, x, packed, scales):
+    """X Q(W)^T of K-major packed codes and scales."""
+    w = F.dequantize(fmt, F.unpack_nibbles(packed), scales)
+    return np.asarray(x, np.float64) @ w.T
+
+
+def token_logprobs(x, targets=None, temperature=1.0, top_k=0):
+    """Dict of logp, stats (max, log sum exp relative to it, entropy), top_logp and top_index."""
+    x = np.asarray(x, np.float64)
+    m, v = x.shape
+    live = np.ones(m, bool) if targets is None else np.asarray(targets) >= 0
+    mx = x.max(1)
+    base = np.where(np.isneginf(mx), 0.0, mx)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        z = (x - base[:, None]) / temperature
+        e = np.exp(z)
+        s = e.sum(1)
+        log_s = np.log(s)
+        logq = z - log_s[:, None]
+        q = e / s[:, None]
+        terms = np.where(q > 0, q * logq, np.where(np.isnan(q), q, 0.0))
+        empty = np.isneginf(mx)
+        ent = np.where(empty, 0.0, -terms.sum(1))
+        out = {"stats": np.where(live[:, None], np.stack([mx, log_s, ent], 1), 0.0)}
+        if targets is not None:
+            t = np.asarray(targets)
+            at = np.clip(t, 0, v - 1)
+            lp = np.where(empty, -np.inf, np.take_along_axis(logq, at[:, None], 1)[:, 0])
+            out["logp"] = np.where(live, np.where(t >= v, np.nan, lp), 0.0)
+        if top_k:
+            k = min(top_k, v)
+            key = np.where(np.isnan(x), -np.inf, x)
+            idx = np.argsort(-key, axis=1, kind="stable")[:, :k]
+            val = np.take_along_axis(logq, idx, 1)
+            gone = np.isneginf(np.take_along_axis(key, idx, 1)) | ~live[:, None]
+            pad = ((0, 0), (0, top_k - k))
+            out["top_logp"] = np.pad(np.where(gone, -np.inf, val), pad, constant_values=-np.inf)
+            out["top_index"] = np.pad(np.where(gone, -1, idx), pad, constant_values=-1).astype(np.int32)
+    return out
+
+
+def token_logprobs_bwd(x, targets, stats, dlogp=None, dentropy=None, temperature=1.0):
+    """Gradient of the logits, with the forward's stats given."""
+    x, stats, t = np.asarray(x, np.float64), np.asarray(stats, np.float64), np.asarray(targets)
+    m, v = x.shape
+    a = np.zeros(m) if dlogp is None else np.asarray(dlogp, np.float64)
+    b = np.zeros(m) if dentropy is None else np.asarray(dentropy, np.float64)
+    zero = (t < 0) | np.isneginf(stats[:, 0])
+    base = np.where(zero, 0.0, stats[:, 0])
+    with np.errstate(invalid="ignore"):
+        logq = (x - base[:, None]) / temperature - np.where(zero, 0.0, stats[:, 1])[:, None]
+        q = np.exp(logq)
+        hot = np.arange(v)[None, :] == t[:, None]
+        g = a[:, None] * (hot - q) - np.where(q > 0, b[:, None] * q * (logq + stats[:, 2:3]), 0.0)
+    g = np.where((t >= v)[:, None], np.nan, g / temperature)
+    return np.where(zero[:, None], 0.0, g)

@@ -278,6 +278,49 @@ int run_activation_side(int format, const Sp& sp, const uint16_t* X, int64_t m, 
   return check_launch("residual/sparsify");
 }
 
+bool valid_dtype(int t) { return t == RESQ_IN_BF16 || t == RESQ_IN_F32; }
+
+// A row-major matrix argument of the operators around the linears: present, aligned to its
+// element, rows at least as far apart as they are long.
+int check_rows(const char* name, const void* p, int dtype, int64_t m, int64_t d, int64_t ld) {
+  if (!valid_dtype(dtype)) return fail(RESQ_ERR_ARG, "unknown %s dtype %d", name, dtype);
+  if (ld < d) return fail(RESQ_ERR_ARG, "ld of %s (%lld) < %lld", name, (long long)ld, (long long)d);
+  if (m == 0 || d == 0) return RESQ_OK;
+  if (!p) return fail(RESQ_ERR_ARG, "%s is NULL", name);
+  if ((uintptr_t)p % (dtype == RESQ_IN_F32 ? 4 : 2) != 0) return fail(RESQ_ERR_ARG, "%s is not aligned to its element", name);
+  return RESQ_OK;
+}
+
+int check_gate(const void* gate, int gate_dtype, int gate_mode) {
+  if (gate_mode != RESQ_GATE_NONE && gate_mode != RESQ_GATE_CHANNEL && gate_mode != RESQ_GATE_TOKEN)
+    return fail(RESQ_ERR_ARG, "unknown gate mode %d", gate_mode);
+  if (gate_mode == RESQ_GATE_NONE) return RESQ_OK;
+  if (!valid_dtype(gate_dtype)) return fail(RESQ_ERR_ARG, "unknown gate dtype %d", gate_dtype);
+  if (!gate || (uintptr_t)gate % (gate_dtype == RESQ_IN_F32 ? 4 : 2) != 0)
+    return fail(RESQ_ERR_ARG, "gate must be non-NULL and aligned to its element");
+  return RESQ_OK;
+}
+
+int check_norm_sizes(int64_t m, int64_t d, float alpha) {
+  if (m < 0 || d < 0) return fail(RESQ_ERR_ARG, "negative size (m=%lld, d=%lld)", (long long)m, (long long)d);
+  if (d > resq::kNormMaxD)
+    return fail(RESQ_ERR_UNSUPPORTED, "the block norm supports d <= %lld (d=%lld)", (long long)resq::kNormMaxD, (long long)d);
+  if (m > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "the block norm supports m < 2^31 (m=%lld)", (long long)m);
+  if (!std::isfinite(alpha)) return fail(RESQ_ERR_ARG, "alpha (%g) must be finite", (double)alpha);
+  return RESQ_OK;
+}
+
+int check_logits(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld, const int64_t* targets,
+                 double temperature) {
+  if (m < 0 || V < 0) return fail(RESQ_ERR_ARG, "negative size (m=%lld, V=%lld)", (long long)m, (long long)V);
+  if (V == 0 && m > 0) return fail(RESQ_ERR_SHAPE, "rows of no logits (V=0)");
+  if (V > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "V (%lld) must be below 2^31", (long long)V);
+  if (!(temperature >= 0x1p-64 && temperature <= 0x1p64))
+    return fail(RESQ_ERR_ARG, "temperature (%g) must lie in [2^-64, 2^64]", temperature);
+  if ((uintptr_t)targets % 8 != 0) return fail(RESQ_ERR_ARG, "targets must be 8-byte aligned");
+  return check_rows("logits", logits, dtype, m, V, ld);
+}
+
 }  // namespace
 
 extern "C" {
@@ -321,6 +364,9 @@ int resq_quantize(int format, const void* x, int in_dtype, int64_t rows, int64_t
 }
 
 size_t resq_workspace_size(int op, int format, int sparsity, int64_t m, int64_t d, int64_t n) {
+  if (m < 0 || d < 0 || n < 0) return 0;
+  if (op == RESQ_OP_BLOCK_NORM_BWD) return resq::norm_bwd_ws_bytes(m, d);
+  if (op == RESQ_OP_TOKEN_LOGPROBS) return n > resq::kMaxTop || d > INT32_MAX ? 0 : resq::logprob_ws_bytes(m, d, (int)n);
   const Sp sp = decode_sparsity(sparsity);
   if (!valid_format(format) || sp.kind < 0 || m < 0 || d < 0 || n < 0) return 0;
   switch (op) {
@@ -769,6 +815,170 @@ int resq_linear_bwd(int format, const uint16_t* dY, const uint16_t* X, const uin
     if (!resq::launch_gemm(op, s)) return fail(RESQ_ERR_UNSUPPORTED, "GEMM operand layout rejected");
   }
   return check_launch("resq_linear_bwd");
+}
+
+int resq_block_norm_fwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_t ldh, const void* Y,
+                        int y_dtype, int64_t ldy, const uint16_t* gamma_post, const void* gate,
+                        int gate_dtype, int gate_mode, float alpha, const uint16_t* gamma_pre,
+                        float eps, void* H_out, int64_t ldho, uint16_t* X, int64_t ldx, float* rstd,
+                        void* stream) {
+  int rc = check_norm_sizes(m, d, alpha);
+  if (rc == RESQ_OK) rc = check_rows("H", H, h_dtype, m, d, ldh);
+  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode);
+  if (rc != RESQ_OK) return rc;
+  if (!std::isfinite(eps) || !(eps >= 0x1p-126f))
+    return fail(RESQ_ERR_ARG, "eps (%g) must be finite and at least 2^-126", (double)eps);
+  if (Y) {
+    rc = check_rows("Y", Y, y_dtype, m, d, ldy);
+    if (rc == RESQ_OK) rc = check_rows("H_out", H_out, h_dtype, m, d, ldho);
+    if (rc != RESQ_OK) return rc;
+  } else if (gamma_post || gate_mode != RESQ_GATE_NONE || !gamma_pre) {
+    return fail(RESQ_ERR_ARG, "without Y there is only the norm of H: gamma_pre, no gamma_post, no gate");
+  }
+  if ((uintptr_t)gamma_post % 2 != 0 || (uintptr_t)gamma_pre % 2 != 0)
+    return fail(RESQ_ERR_ARG, "gamma_post and gamma_pre must be 2-byte aligned");
+  if (gamma_pre) {
+    rc = check_rows("X", X, RESQ_IN_BF16, m, d, ldx);
+    if (rc != RESQ_OK) return rc;
+  }
+  if ((uintptr_t)rstd % 4 != 0) return fail(RESQ_ERR_ARG, "rstd must be 4-byte aligned");
+  if (m == 0 || d == 0) return ok();
+  const resq::NormFwd p{H, Y, gamma_post, gate, gamma_pre, H_out, X, rstd, m, d, ldh, ldy, ldho, ldx,
+                        alpha, eps, gate_mode, gate_dtype == RESQ_IN_F32};
+  const hipStream_t s = (hipStream_t)stream;
+  {
+    resq::ProfScope prof_(resq::kProfNorm, s, true);
+    resq::launch_norm_fwd(p, h_dtype == RESQ_IN_F32, y_dtype == RESQ_IN_F32, s);
+  }
+  return check_launch("resq_block_norm_fwd");
+}
+
+int resq_block_norm_bwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_t ldh, const void* Y,
+                        int y_dtype, int64_t ldy, const uint16_t* gamma_post, const void* gate,
+                        int gate_dtype, int gate_mode, float alpha, const uint16_t* gamma_pre,
+                        const float* rstd, const void* dX, int dx_dtype, int64_t lddx, const void* dH_out,
+                        int64_t lddho, void* dH, int64_t lddh, void* dY, int dy_dtype, int64_t lddy,
+                        float* dgamma_post, float* dgamma_pre, float* dgate, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int rc = check_norm_sizes(m, d, alpha);
+  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode);
+  if (rc != RESQ_OK) return rc;
+  if (!valid_dtype(h_dtype)) return fail(RESQ_ERR_ARG, "unknown H dtype %d", h_dtype);
+  if (!dH && !dY && !dgamma_post && !dgamma_pre && !dgate) return fail(RESQ_ERR_ARG, "no gradient is wanted");
+  if (dgamma_post && !gamma_post) return fail(RESQ_ERR_ARG, "dgamma_post without gamma_post");
+  if (dgamma_pre && !gamma_pre) return fail(RESQ_ERR_ARG, "dgamma_pre without gamma_pre");
+  if (dgate && gate_mode == RESQ_GATE_NONE) return fail(RESQ_ERR_ARG, "dgate without a gate");
+  if ((uintptr_t)gamma_post % 2 != 0 || (uintptr_t)gamma_pre % 2 != 0)
+    return fail(RESQ_ERR_ARG, "gamma_post and gamma_pre must be 2-byte aligned");
+  if ((uintptr_t)rstd % 4 != 0 || (uintptr_t)dgamma_post % 4 != 0 || (uintptr_t)dgamma_pre % 4 != 0 || (uintptr_t)dgate % 4 != 0)
+    return fail(RESQ_ERR_ARG, "rstd, dgamma_post, dgamma_pre and dgate must be 4-byte aligned");
+  // Y is read by the gradients through the norm after the block and by the gate's
+  const bool need_y = (gamma_post && (dY || dgamma_post)) || dgate;
+  if (need_y) rc = check_rows("Y", Y, y_dtype, m, d, ldy);
+  if (rc == RESQ_OK && gamma_pre) rc = check_rows("H", H, h_dtype, m, d, ldh);
+  if (rc == RESQ_OK && gamma_pre) rc = check_rows("dX", dX, dx_dtype, m, d, lddx);
+  if (rc == RESQ_OK && dH_out) rc = check_rows("dH_out", dH_out, h_dtype, m, d, lddho);
+  if (rc == RESQ_OK && dH) rc = check_rows("dH", dH, h_dtype, m, d, lddh);
+  if (rc == RESQ_OK && dY) rc = check_rows("dY", dY, dy_dtype, m, d, lddy);
+  if (rc != RESQ_OK) return rc;
+  const hipStream_t s = (hipStream_t)stream;
+  if (d == 0) {
+    if (dgate && gate_mode == RESQ_GATE_TOKEN) resq::launch_zero_f32(dgate, m, s);
+    return check_launch("resq_block_norm_bwd");
+  }
+  if (m == 0) {  // sums over no rows
+    if (dgamma_post) resq::launch_zero_f32(dgamma_post, d, s);
+    if (dgamma_pre) resq::launch_zero_f32(dgamma_pre, d, s);
+    if (dgate && gate_mode == RESQ_GATE_CHANNEL) resq::launch_zero_f32(dgate, d, s);
+    return check_launch("resq_block_norm_bwd");
+  }
+  if ((gamma_pre || gamma_post) && !rstd) return fail(RESQ_ERR_ARG, "rstd is NULL");
+  rc = check_ws(workspace, workspace_bytes, resq::norm_bwd_ws_bytes(m, d));
+  if (rc != RESQ_OK) return rc;
+  resq::NormBwd p{};
+  p.h = H; p.y = need_y ? Y : nullptr; p.dx = dX; p.dho = dH_out;
+  p.gamma_post = gamma_post; p.gate = gate; p.gamma_pre = gamma_pre; p.rstd = rstd;
+  p.dh = dH; p.dy = dY; p.dgate = dgate;
+  p.m = m; p.d = d; p.ldh = ldh; p.ldy = ldy; p.lddx = lddx; p.lddho = lddho; p.lddh = lddh; p.lddy = lddy;
+  p.alpha = alpha; p.gate_mode = gate_mode; p.gate_f32 = gate_dtype == RESQ_IN_F32; p.dy_f32 = dy_dtype == RESQ_IN_F32;
+  {
+    resq::ProfScope prof_(resq::kProfNorm, s, true);
+    resq::launch_norm_bwd(p, h_dtype == RESQ_IN_F32, y_dtype == RESQ_IN_F32, dx_dtype == RESQ_IN_F32, dgamma_post,
+                          dgamma_pre, (float*)workspace, s);
+  }
+  return check_launch("resq_block_norm_bwd");
+}
+
+int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64_t ldx,
+                      const uint8_t* qw_codes, const void* qw_scales, int64_t n, void* Y, int y_dtype,
+                      int64_t ldy, void* stream) {
+  if (!valid_format(format)) return fail(RESQ_ERR_ARG, "unknown format %d", format);
+  if (m < 0 || d < 0 || n < 0) return fail(RESQ_ERR_ARG, "negative size");
+  if (d % block_of(format) != 0)
+    return fail(RESQ_ERR_SHAPE, "d (%lld) is not a multiple of the block size %lld", (long long)d, (long long)block_of(format));
+  int rc = check_rows("X", X, RESQ_IN_BF16, m, d, ldx);
+  if (rc == RESQ_OK) rc = check_rows("Y", Y, y_dtype, m, n, ldy);
+  if (rc != RESQ_OK) return rc;
+  if (m > resq::kMatvecMaxRows)
+    return fail(RESQ_ERR_UNSUPPORTED, "m (%lld) > %lld: use resq_linear_w4a16", (long long)m, (long long)resq::kMatvecMaxRows);
+  if (n > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "n (%lld) must be below 2^31", (long long)n);
+  if (m == 0 || n == 0) return ok();
+  if (d > 0 && (!qw_codes || !qw_scales || (uintptr_t)qw_codes % 16 != 0 ||
+                (format == RESQ_HIF4 && (uintptr_t)qw_scales % 4 != 0)))
+    return fail(RESQ_ERR_ARG, "qw_codes must be 16-byte aligned (HiF4 scales 4-byte aligned)");
+  const hipStream_t s = (hipStream_t)stream;
+  {
+    resq::ProfScope prof_(resq::kProfMatvec, s, true);
+    resq::launch_matvec(format, X, m, d, ldx, qw_codes, qw_scales, n, Y, ldy, y_dtype == RESQ_IN_BF16, s);
+  }
+  return check_launch("resq_matvec_w4a16");
+}
+
+int resq_token_logprobs(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld,
+                        const int64_t* targets, double temperature, float* logp, float* stats,
+                        int top_k, float* top_logp, int32_t* top_index, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  int rc = check_logits(logits, dtype, m, V, ld, targets, temperature);
+  if (rc != RESQ_OK) return rc;
+  if (top_k < 0 || top_k > resq::kMaxTop)
+    return fail(RESQ_ERR_ARG, "top_k (%d) must lie in 0..%d", top_k, resq::kMaxTop);
+  if (m > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "m (%lld) must be below 2^31", (long long)m);
+  if (m == 0) return ok();
+  if (logp && !targets) return fail(RESQ_ERR_ARG, "logp without targets");
+  if (!stats) return fail(RESQ_ERR_ARG, "stats is NULL");
+  if (top_k > 0 && (!top_logp || !top_index)) return fail(RESQ_ERR_ARG, "top_logp / top_index is NULL");
+  if ((uintptr_t)logp % 4 != 0 || (uintptr_t)stats % 4 != 0 || (uintptr_t)top_logp % 4 != 0 || (uintptr_t)top_index % 4 != 0)
+    return fail(RESQ_ERR_ARG, "logp, stats, top_logp and top_index must be 4-byte aligned");
+  rc = check_ws(workspace, workspace_bytes, resq::logprob_ws_bytes(m, V, top_k));
+  if (rc != RESQ_OK) return rc;
+  const resq::LogprobFwd p{logits, m, V, ld, targets, temperature, logp, stats, top_k, top_logp, top_index};
+  const hipStream_t s = (hipStream_t)stream;
+  {
+    resq::ProfScope prof_(resq::kProfLogprob, s, true);
+    resq::launch_logprob_fwd(p, dtype == RESQ_IN_F32, workspace, s);
+  }
+  return check_launch("resq_token_logprobs");
+}
+
+int resq_token_logprobs_bwd(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld,
+                            const int64_t* targets, double temperature, const float* stats,
+                            const float* dlogp, const float* dentropy, void* dlogits, int out_dtype,
+                            int64_t ldd, void* stream) {
+  int rc = check_logits(logits, dtype, m, V, ld, targets, temperature);
+  if (rc == RESQ_OK) rc = check_rows("dlogits", dlogits, out_dtype, m, V, ldd);
+  if (rc != RESQ_OK) return rc;
+  if (m == 0) return ok();
+  if (!targets || !stats) return fail(RESQ_ERR_ARG, "targets / stats is NULL");
+  if ((uintptr_t)stats % 4 != 0 || (uintptr_t)dlogp % 4 != 0 || (uintptr_t)dentropy % 4 != 0)
+    return fail(RESQ_ERR_ARG, "stats, dlogp and dentropy must be 4-byte aligned");
+  if (!resq::logprob_bwd_supported(m, V)) return fail(RESQ_ERR_UNSUPPORTED, "m * V too large for one launch");
+  const resq::LogprobBwd p{logits, m, V, ld, targets, temperature, stats, dlogp, dentropy, dlogits, ldd};
+  const hipStream_t s = (hipStream_t)stream;
+  {
+    resq::ProfScope prof_(resq::kProfLogprob, s, true);
+    resq::launch_logprob_bwd(p, dtype == RESQ_IN_F32, out_dtype == RESQ_IN_F32, s);
+  }
+  return check_launch("resq_token_logprobs_bwd");
 }
 
 }  // extern "C"

@@ -167,6 +167,83 @@ void launch_quant_rows_bf16(int fmt, const uint16_t* x, int64_t rows, int64_t co
 // p[0 .. n) = 0 (a fill kernel: callers may capture the library's launches in a graph).
 void launch_zero_f32(float* p, int64_t n, hipStream_t s);
 
+// Norms before and after a block with its gate, residual scale and residual addition (norm.hip):
+// the row kernels' arguments, as resq_block_norm_fwd / _bwd describe them.  Widths up to
+// kNormMaxD (a row is held in one workgroup's registers).
+constexpr int64_t kNormMaxD = 16384;
+enum GateMode { kGateNone = 0, kGateChannel = 1, kGateToken = 2 };
+struct NormFwd {
+  const void* h;
+  const void* y;               // null: only the norm of h
+  const uint16_t* gamma_post;  // null: no norm of y
+  const void* gate;
+  const uint16_t* gamma_pre;   // null: no norm of h'
+  void* h_out;
+  uint16_t* x;
+  float* rstd;                 // [2][m], or null
+  int64_t m, d, ldh, ldy, ldho, ldx;
+  float alpha, eps;
+  int gate_mode;
+  bool gate_f32;
+};
+void launch_norm_fwd(const NormFwd& p, bool h_f32, bool y_f32, hipStream_t s);
+struct NormBwd {
+  const void* h;               // the stored h'
+  const void* y;               // null where no gradient needs it
+  const void* dx;              // gradient of x (read when gamma_pre is not null)
+  const void* dho;             // gradient of h', or null
+  const uint16_t* gamma_post;
+  const void* gate;
+  const uint16_t* gamma_pre;
+  const float* rstd;
+  void* dh;                    // outputs; null: not wanted
+  void* dy;
+  float* dgate;
+  int64_t m, d, ldh, ldy, lddx, lddho, lddh, lddy;
+  float alpha;
+  int gate_mode;
+  bool gate_f32, dy_f32;
+  float *part_pre, *part_post, *part_gate;  // set by launch_norm_bwd
+};
+size_t norm_bwd_ws_bytes(int64_t m, int64_t d);
+void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgamma_post, float* dgamma_pre,
+                     float* workspace, hipStream_t s);
+
+// A few rows of bf16 activations (m <= kMatvecMaxRows) times 4-bit weights (matvec.hip):
+// Y[m][n] = X[m][d] Q(W)[n][d]^T, Y float32 or bf16.
+constexpr int64_t kMatvecMaxRows = 16;
+void launch_matvec(int fmt, const uint16_t* X, int64_t m, int64_t d, int64_t ldx, const uint8_t* codes,
+                   const void* scales, int64_t n, void* Y, int64_t ldy, bool out_bf16, hipStream_t s);
+
+// Token log probabilities (logprob.hip), as resq_token_logprobs / _bwd describe them.
+constexpr int kMaxTop = 32;
+struct LogprobFwd {
+  const void* logits;
+  int64_t m, V, ld;
+  const int64_t* targets;  // null: none
+  double temperature;
+  float* logp;             // null: not wanted
+  float* stats;
+  int top_k;
+  float* top_logp;
+  int32_t* top_index;
+};
+size_t logprob_ws_bytes(int64_t m, int64_t V, int top_k);
+void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStream_t s);
+struct LogprobBwd {
+  const void* logits;
+  int64_t m, V, ld;
+  const int64_t* targets;
+  double temperature;
+  const float* stats;
+  const float* dlogp;      // null: zero
+  const float* dentropy;   // null: zero
+  void* dlogits;
+  int64_t ldd;
+};
+bool logprob_bwd_supported(int64_t m, int64_t V);  // the grid fits a launch
+void launch_logprob_bwd(const LogprobBwd& p, bool f32, bool out_f32, hipStream_t s);
+
 // Activation statistics (diag.hip): stats receives 9 doubles (see resq_diagnostics);
 // partials is diag_ws_bytes(m, d) bytes of scratch.
 size_t diag_ws_bytes(int64_t m, int64_t d);

@@ -75,6 +75,10 @@ NOALLOC_SCRATCH_BYTES = 64 << 20  # RESQ_NOALLOC_SCRATCH_BYTES
 OP_RESIDUAL_SPARSIFY, OP_LINEAR_FWD, OP_LINEAR_BWD, OP_LINEAR_FWD_PREPARED, OP_DIAGNOSTICS = 0, 1, 2, 3, 4
 OP_LINEAR_W16A4 = 5
 OP_LINEAR_FWD_RMSNORM = 6
+OP_BLOCK_NORM_BWD, OP_TOKEN_LOGPROBS = 7, 8
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
+MATVEC_MAX_ROWS = 16
+MAX_TOP_K = 32
 DIAG_STATS = ("elements", "zeros_x", "zeros_qx", "blocks", "outlier_blocks", "energy_qx",
               "sse24_qx", "energy_qr", "sse24_qr")
 
@@ -84,7 +88,8 @@ EXPORTED = ("resq_quantize", "resq_residual_sparsify", "resq_linear_fwd", "resq_
             "resq_prepare_weights", "resq_linear_fwd_prepared", "resq_linear_fwd_prepared_bf16",
             "resq_diagnostics", "resq_linear_fwd_prepared_swiglu", "resq_gemm_plan",
             "resq_linear_fwd_prepared_noalloc", "resq_linear_w4a16", "resq_linear_w16a4",
-            "resq_linear_fwd_prepared_rmsnorm")
+            "resq_linear_fwd_prepared_rmsnorm", "resq_block_norm_fwd", "resq_block_norm_bwd",
+            "resq_matvec_w4a16", "resq_token_logprobs", "resq_token_logprobs_bwd")
 GEMM_TILES = {0: "64x64", 1: "128x256", 2: "128x192", 3: "128x192_8w", 4: "64x128", 5: "32x32", 6: "32x64",
               7: "32x96"}
 
@@ -151,6 +156,17 @@ def load() -> ctypes.CDLL:
     lib.resq_linear_w4a16.restype = i32
     lib.resq_linear_w16a4.argtypes = [i32, vp, i64, i64, i64, vp, i64, i64, vp, i64, vp, sz, vp]
     lib.resq_linear_w16a4.restype = i32
+    f32, f64 = ctypes.c_float, ctypes.c_double
+    lib.resq_block_norm_fwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, vp, i32, i32, f32, vp, f32, vp, i64,
+                                        vp, i64, vp, vp]
+    lib.resq_block_norm_bwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, vp, vp, i32, i32, f32, vp, vp, vp, i32,
+                                        i64, vp, i64, vp, i64, vp, i32, i64, vp, vp, vp, vp, sz, vp]
+    lib.resq_matvec_w4a16.argtypes = [i32, vp, i64, i64, i64, vp, vp, i64, vp, i32, i64, vp]
+    lib.resq_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, f64, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.resq_token_logprobs_bwd.argtypes = [vp, i32, i64, i64, i64, vp, f64, vp, vp, vp, vp, i32, i64, vp]
+    for f in ("resq_block_norm_fwd", "resq_block_norm_bwd", "resq_matvec_w4a16", "resq_token_logprobs",
+              "resq_token_logprobs_bwd"):
+        getattr(lib, f).restype = i32
     lib.resq_gemm_plan.argtypes = [i32, i64, i64, i64, i32, ctypes.POINTER(ctypes.c_int32)]
     lib.resq_gemm_plan.restype = i32
     lib.resq_last_error.restype = ctypes.c_char_p
@@ -232,6 +248,37 @@ def resq_diagnostics(fmt, X, m, d, ldx, outlier_threshold, stats, workspace, wor
                      stream=0) -> int:
     return load().resq_diagnostics(fmt, X, m, d, ldx, outlier_threshold, stats, workspace,
                                    workspace_bytes, stream)
+
+
+def resq_block_norm_fwd(H, h_dtype, m, d, ldh, Y, y_dtype, ldy, gamma_post, gate, gate_dtype, gate_mode, alpha,
+                        gamma_pre, eps, H_out, ldho, X, ldx, rstd, stream=0) -> int:
+    return load().resq_block_norm_fwd(H, h_dtype, m, d, ldh, Y, y_dtype, ldy, gamma_post, gate, gate_dtype, gate_mode,
+                                      alpha, gamma_pre, eps, H_out, ldho, X, ldx, rstd, stream)
+
+
+def resq_block_norm_bwd(H, h_dtype, m, d, ldh, Y, y_dtype, ldy, gamma_post, gate, gate_dtype, gate_mode, alpha,
+                        gamma_pre, rstd, dX, dx_dtype, lddx, dH_out, lddho, dH, lddh, dY, dy_dtype, lddy,
+                        dgamma_post, dgamma_pre, dgate, workspace, workspace_bytes, stream=0) -> int:
+    return load().resq_block_norm_bwd(H, h_dtype, m, d, ldh, Y, y_dtype, ldy, gamma_post, gate, gate_dtype, gate_mode,
+                                      alpha, gamma_pre, rstd, dX, dx_dtype, lddx, dH_out, lddho, dH, lddh, dY,
+                                      dy_dtype, lddy, dgamma_post, dgamma_pre, dgate, workspace, workspace_bytes,
+                                      stream)
+
+
+def resq_matvec_w4a16(fmt, X, m, d, ldx, qw_codes, qw_scales, n, Y, y_dtype, ldy, stream=0) -> int:
+    return load().resq_matvec_w4a16(fmt, X, m, d, ldx, qw_codes, qw_scales, n, Y, y_dtype, ldy, stream)
+
+
+def resq_token_logprobs(logits, dtype, m, V, ld, targets, temperature, logp, stats, top_k, top_logp, top_index,
+                        workspace, workspace_bytes, stream=0) -> int:
+    return load().resq_token_logprobs(logits, dtype, m, V, ld, targets, temperature, logp, stats, top_k, top_logp,
+                                      top_index, workspace, workspace_bytes, stream)
+
+
+def resq_token_logprobs_bwd(logits, dtype, m, V, ld, targets, temperature, stats, dlogp, dentropy, dlogits, out_dtype,
+                            ldd, stream=0) -> int:
+    return load().resq_token_logprobs_bwd(logits, dtype, m, V, ld, targets, temperature, stats, dlogp, dentropy,
+                                          dlogits, out_dtype, ldd, stream)
 
 
 def resq_gemm_plan(fmt, M, N, K, split_allowed, info) -> int:
@@ -518,3 +565,279 @@ def linear_fwd_swiglu(g, u, wprep, n, fmt, sparsity, y=None, ws=None, stream=Non
                                          _p(wprep), n, _p(y), y.stride(0), _p(buf), nb, _stream(stream))
     _check(rc, "resq_linear_fwd_prepared_swiglu")
     return y
+
+
+# ------------------------------------------------------------------------------------------
+# operators around the linears
+# ------------------------------------------------------------------------------------------
+def _dtype(t, what) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return IN_F32
+    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
+        return IN_BF16
+    raise TypeError(f"{what} must be float32 or bfloat16 (or its 16-bit patterns), not {t.dtype}")
+
+
+def _like(dtype_code):
+    import torch
+    return torch.float32 if dtype_code == IN_F32 else torch.bfloat16
+
+
+def _out_code(out) -> int:
+    if out not in ("f32", "bf16"):
+        raise ValueError(f"out must be 'f32' or 'bf16', not {out!r}")
+    return IN_F32 if out == "f32" else IN_BF16
+
+
+def _rows(t, what, m, d, dev) -> int:
+    """The row stride of an m x d device matrix with unit column stride."""
+    if t.device != dev:
+        raise ValueError(f"{what} is on {t.device}, not on {dev}")
+    if t.dim() != 2 or t.shape[0] != m or t.shape[1] != d:
+        raise ValueError(f"{what} must be {m} x {d}, not {tuple(t.shape)}")
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have unit column stride")
+    if m <= 1:
+        return d
+    if t.stride(0) < d:
+        raise ValueError(f"{what} has overlapping rows (stride {t.stride(0)} < {d})")
+    return t.stride(0)
+
+
+def _vector(t, what, n, dtypes, dev):
+    if t is None:
+        return 0
+    if t.device != dev:
+        raise ValueError(f"{what} is on {t.device}, not on {dev}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} has type {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must hold {n} contiguous values")
+    return t.data_ptr()
+
+
+class _On:
+    """The device and stream a call runs on: `stream`, or the current one of the tensor's device.
+    Inside, torch allocates for that stream."""
+
+    def __init__(self, t, stream):
+        import torch
+        if t.device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, not on {t.device}")
+        self.ctx = None
+        if stream is not None:
+            if stream.device != t.device:
+                raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+            self.ctx = torch.cuda.stream(stream)
+        elif t.device.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(t.device)
+
+    def __enter__(self):
+        import torch
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _workspace(op, m, d, n, dev):
+    """(tensor, pointer, bytes): allocated on the current stream."""
+    import torch
+    nb = load().resq_workspace_size(op, 0, 0, m, d, n)
+    t = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    return t, _p(t), nb
+
+
+def _ws_arg(ws, op, m, d, n, dev):
+    if ws is None:
+        return _workspace(op, m, d, n, dev)
+    buf, nb = ws
+    if buf.device != dev:
+        raise ValueError(f"the workspace is on {buf.device}, not on {dev}")
+    return buf, _p(buf), nb
+
+
+def _gate_args(gate, m, d, dev):
+    """(pointer, dtype, mode): d values (or 1 x d) per channel, m x 1 per token."""
+    if gate is None:
+        return 0, IN_BF16, GATE_NONE
+    if gate.device != dev:
+        raise ValueError(f"gate is on {gate.device}, not on {dev}")
+    if not gate.is_contiguous():
+        raise ValueError("gate must be contiguous")
+    shape = tuple(gate.shape)
+    if shape == (d,) or (shape == (1, d) and not (m == 1 and d == 1)):
+        return gate.data_ptr(), _dtype(gate, "gate"), GATE_CHANNEL
+    if shape == (m, 1):
+        return gate.data_ptr(), _dtype(gate, "gate"), GATE_TOKEN
+    raise ValueError(f"gate must have shape ({d},) or ({m}, 1), not {shape}")
+
+
+def block_norm(h, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None, eps=1e-6, save=True, h_out=None,
+               x=None, stream=None):
+    """The residual update after a block, with the norms around it:
+        h_out = h + alpha * gate * (RMSNorm(y) * gamma_post),   x = RMSNorm(h_out) * gamma_pre
+    h and y are m x d (bfloat16 or float32), gamma_post and gamma_pre d bfloat16 values (None: no
+    norm there), gate d values (per channel) or m x 1 (per token).  h_out may be h (in place).
+    Returns (h_out, x, rstd): x bfloat16 (None without gamma_pre), rstd the 2 x m row factors that
+    block_norm_bwd takes (None with save=False).  Without y: the norm of h alone, h_out is h."""
+    import torch
+    if h.dim() != 2:
+        raise ValueError("h must be a matrix")
+    m, d = h.shape
+    dev = h.device
+    bits = (torch.bfloat16, torch.int16, torch.uint16)
+    hd, ldh = _dtype(h, "h"), _rows(h, "h", m, d, dev)
+    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, dev))
+    g, gd, gm = _gate_args(gate, m, d, dev)
+    gpost, gpre = _vector(gamma_post, "gamma_post", d, bits, dev), _vector(gamma_pre, "gamma_pre", d, bits, dev)
+    with _On(h, stream) as s:
+        if y is None:
+            h_out = h
+        elif h_out is None:
+            h_out = torch.empty((m, d), dtype=h.dtype, device=dev)
+        elif h_out.dtype != h.dtype:
+            raise TypeError(f"h_out has type {h_out.dtype}, h {h.dtype}")
+        ldho = _rows(h_out, "h_out", m, d, dev)
+        if gamma_pre is None:
+            x, ldx = None, d
+        elif x is None:
+            x, ldx = torch.empty((m, d), dtype=torch.bfloat16, device=dev), d
+        else:
+            if _dtype(x, "x") != IN_BF16:
+                raise TypeError("x must be bfloat16")
+            ldx = _rows(x, "x", m, d, dev)
+        rstd = torch.empty((2, m), dtype=torch.float32, device=dev) if save else None
+        rc = resq_block_norm_fwd(h.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, eps,
+                                 h_out.data_ptr(), ldho, _p(x), ldx, _p(rstd), s)
+    _check(rc, "resq_block_norm_fwd")
+    return h_out, x, rstd
+
+
+def block_norm_bwd(h_out, rstd, dx=None, dh=None, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None,
+                   out="bf16", want_dh=True, want_dy=True, ws=None, stream=None):
+    """Gradients of block_norm: dx and dh are those of its x and h_out (None: zero; dx goes with
+    gamma_pre), the other arguments the forward's and rstd its output.  Returns a dict of dh (of
+    h), dy (`out` type), dgamma_post, dgamma_pre and dgate (float32; None where there is none)."""
+    import torch
+    if h_out.dim() != 2:
+        raise ValueError("h_out must be a matrix")
+    m, d = h_out.shape
+    dev = h_out.device
+    bits = (torch.bfloat16, torch.int16, torch.uint16)
+    hd, ldh = _dtype(h_out, "h_out"), _rows(h_out, "h_out", m, d, dev)
+    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, dev))
+    xd, lddx = (IN_BF16, d) if dx is None else (_dtype(dx, "dx"), _rows(dx, "dx", m, d, dev))
+    lddho = d
+    if dh is not None:
+        if _dtype(dh, "dh") != hd:
+            raise TypeError(f"dh has type {dh.dtype}, h_out {h_out.dtype}")
+        lddho = _rows(dh, "dh", m, d, dev)
+    g, gd, gm = _gate_args(gate, m, d, dev)
+    gpost, gpre = _vector(gamma_post, "gamma_post", d, bits, dev), _vector(gamma_pre, "gamma_pre", d, bits, dev)
+    rs = _vector(rstd, "rstd", 2 * m, (torch.float32,), dev)
+    yt = _out_code(out)
+    with _On(h_out, stream) as s:
+        def empty(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=dev)
+        r = {"dh": empty(m, d, dtype=_like(hd)) if want_dh else None,
+             "dy": empty(m, d, dtype=_like(yt)) if want_dy else None,
+             "dgamma_post": empty(d) if gamma_post is not None else None,
+             "dgamma_pre": empty(d) if gamma_pre is not None else None,
+             "dgate": None if gate is None else empty(*gate.shape)}
+        keep, wp, nb = _ws_arg(ws, OP_BLOCK_NORM_BWD, m, d, 0, dev)
+        rc = resq_block_norm_bwd(h_out.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, rs,
+                                 _p(dx), xd, lddx, _p(dh), lddho, _p(r["dh"]), d, _p(r["dy"]), yt, d,
+                                 _p(r["dgamma_post"]), _p(r["dgamma_pre"]), _p(r["dgate"]), wp, nb, s)
+    _check(rc, "resq_block_norm_bwd")
+    return r
+
+
+def matvec_w4a16(x, qw_codes, qw_scales, fmt, out="f32", y=None, stream=None):
+    """Y = X Q(W)^T for at most MATVEC_MAX_ROWS rows of bfloat16 x (linear_w4a16 for more): float32,
+    or with out="bf16" rounded to bfloat16."""
+    import torch
+    f = _fmt(fmt)
+    if x.dim() != 2 or qw_codes.dim() != 2:
+        raise ValueError("x and qw_codes must be matrices")
+    m, d = x.shape
+    n = qw_codes.shape[0]
+    dev = x.device
+    if _dtype(x, "x") != IN_BF16:
+        raise TypeError("x must be bfloat16")
+    ldx = _rows(x, "x", m, d, dev)
+    if qw_codes.shape[1] * 2 != d:
+        raise ValueError(f"qw_codes hold rows of {qw_codes.shape[1] * 2}, x of {d}")
+    shape, _ = scale_shape(f, n, d)
+    cp = _vector(qw_codes, "qw_codes", n * (d // 2), (torch.uint8,), dev)
+    sp = _vector(qw_scales, "qw_scales", shape[0] * shape[1],
+                 (torch.uint8,) if f == MXFP4 else (torch.int32, torch.uint32), dev)
+    yt = _out_code(out)
+    with _On(x, stream) as s:
+        if y is None:
+            y, ldy = torch.empty((m, n), dtype=_like(yt), device=dev), n
+        else:
+            if _dtype(y, "y") != yt:
+                raise TypeError(f"y has type {y.dtype}, out is {out!r}")
+            ldy = _rows(y, "y", m, n, dev)
+        rc = resq_matvec_w4a16(f, x.data_ptr(), m, d, ldx, cp, sp, n, y.data_ptr(), yt, ldy, s)
+    _check(rc, "resq_matvec_w4a16")
+    return y
+
+
+def token_logprobs(logits, targets=None, temperature=1.0, top_k=0, ws=None, stream=None):
+    """Log probabilities of the targets (m int64 token numbers; negative: none) under m x V logits
+    (float32 or bfloat16) at a temperature.  Returns a dict: logp (m; with targets), stats (m x 3:
+    the largest logit, log sum exp relative to it, the entropy) and, with top_k, top_logp and
+    top_index (m x top_k, int32)."""
+    import torch
+    if logits.dim() != 2:
+        raise ValueError("logits must be a matrix")
+    m, v = logits.shape
+    dev = logits.device
+    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, dev)
+    tp = _vector(targets, "targets", m, (torch.int64,), dev)
+    top_k = int(top_k)
+    with _On(logits, stream) as s:
+        r = {} if targets is None else {"logp": torch.empty(m, dtype=torch.float32, device=dev)}
+        r["stats"] = torch.empty((m, 3), dtype=torch.float32, device=dev)
+        if top_k > 0:
+            r["top_logp"] = torch.empty((m, top_k), dtype=torch.float32, device=dev)
+            r["top_index"] = torch.empty((m, top_k), dtype=torch.int32, device=dev)
+        keep, wp, nb = _ws_arg(ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
+        rc = resq_token_logprobs(logits.data_ptr(), dt, m, v, ld, tp, temperature, _p(r.get("logp")),
+                                 r["stats"].data_ptr(), top_k, _p(r.get("top_logp")), _p(r.get("top_index")), wp, nb, s)
+    _check(rc, "resq_token_logprobs")
+    return r
+
+
+def token_logprobs_bwd(logits, targets, stats, dlogp=None, dentropy=None, temperature=1.0, out="bf16", dlogits=None,
+                       stream=None):
+    """The gradient of the logits from those of token_logprobs' logp (dlogp) and of the entropy
+    stats[:, 2] (dentropy), either None for zero: m x V of type `out`.  stats is token_logprobs';
+    dlogits may be logits (in place) when the types are equal."""
+    import torch
+    if logits.dim() != 2:
+        raise ValueError("logits must be a matrix")
+    m, v = logits.shape
+    dev = logits.device
+    f32 = (torch.float32,)
+    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, dev)
+    tp, st = _vector(targets, "targets", m, (torch.int64,), dev), _vector(stats, "stats", 3 * m, f32, dev)
+    da, db = _vector(dlogp, "dlogp", m, f32, dev), _vector(dentropy, "dentropy", m, f32, dev)
+    ot = _out_code(out)
+    with _On(logits, stream) as s:
+        if dlogits is None:
+            dlogits, ldd = torch.empty((m, v), dtype=_like(ot), device=dev), v
+        else:
+            if _dtype(dlogits, "dlogits") != ot:
+                raise TypeError(f"dlogits has type {dlogits.dtype}, out is {out!r}")
+            ldd = _rows(dlogits, "dlogits", m, v, dev)
+        rc = resq_token_logprobs_bwd(logits.data_ptr(), dt, m, v, ld, tp, temperature, st, da, db, dlogits.data_ptr(),
+                                     ot, ldd, s)
+    _check(rc, "resq_token_logprobs_bwd")
+    return dlogits
