@@ -203,7 +203,7 @@ struct NormBwd {
   float alpha;
   int gate_mode;
   bool gate_f32, dy_f32;
-  float *part_pre, *part_post, *part_gate;  // set by launch_norm_bwd
+  float *part_pre, *part_branch;  // set by launch_norm_bwd
 };
 size_t norm_bwd_ws_bytes(int64_t m, int64_t d);
 void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgamma_post, float* dgamma_pre,

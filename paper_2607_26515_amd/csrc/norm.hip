@@ -6,10 +6,17 @@
 //   x = h' r_h gamma_pre           of the stored h'
 //
 // Both are bound by HBM: each row is read once and kept in registers between its statistics and
-// its use.  A row belongs to L lanes of one workgroup, each holding C groups of eight consecutive
-// elements; L <= 64 shares a workgroup between several rows.
+// its use.  A row belongs to L lanes of one workgroup, each holding C groups of E = 8 consecutive
+// elements (E = 1 for rows shorter than 8).  L < 64: several rows share a wave.
+//
+// A row's last group is moved back to end at the row's end, so that every lane's accesses are
+// whole (a lane past the end takes the same place): the elements that two lanes then hold count
+// once in a row sum (`skip` elements are left out) and get the same value from both.  In-place
+// calls stay right because every lane's loads come before any store: within a wave by program
+// order, across waves by the barrier of a row sum, or one of their own where there is no sum.
 #include <algorithm>
 
+#include "device_fp4.h"
 #include "kernels.h"
 #include "ops_core.h"
 #include "profiler.h"
@@ -19,27 +26,63 @@ namespace {
 
 constexpr int kMaxWaves = 16;
 
-// Sum of N values per lane over the L lanes of a row (L a power of two up to 64, or a multiple of
-// 64: then the whole workgroup is one row and lds holds N * kMaxWaves values).  Every lane gets
-// the sum; the order is fixed.  Barriers: one (L > 64); lds must not be in use by an earlier call.
+// A value from another lane of the same 16 (DPP; both halves of a double), and the sum with the
+// lanes 16 or 32 away (gfx950's half swaps).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __uint_as_float(dpp_u32<CTRL>(__float_as_uint(v))); }
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, ((uint64_t)dpp_u32<CTRL>((uint32_t)(u >> 32)) << 32) | dpp_u32<CTRL>((uint32_t)u));
+}
+template <bool HALF>
+__device__ __forceinline__ u32x2 swap_rows(uint32_t v) {
+  if constexpr (HALF) return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+  else return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+}
+template <bool HALF>
+__device__ __forceinline__ float add_swapped(float v) {
+  const u32x2 r = swap_rows<HALF>(__float_as_uint(v));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <bool HALF>
+__device__ __forceinline__ double add_swapped(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const u32x2 lo = swap_rows<HALF>((uint32_t)u), hi = swap_rows<HALF>((uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, ((uint64_t)hi[0] << 32) | lo[0]) +
+         __builtin_bit_cast(double, ((uint64_t)hi[1] << 32) | lo[1]);
+}
+
+// Sum of N values per lane over the L lanes of a row (L a power of two up to 32, or a multiple of
+// 64: then, past 64, the whole workgroup is one row).  Every lane gets the sum; the order is fixed.
+// Barriers: one (L > 64).  lds: N * kMaxWaves values, zero beyond the row's waves, not in use by
+// an earlier call.
 template <int N, typename T>
 __device__ __forceinline__ void row_sum(T v[N], int L, T* lds) {
-  const int width = L < 64 ? L : 64;
-  for (int o = 1; o < width; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], o, 64);
+#define RESQ_STEP(MIN, EXPR)                    \
+  if (L >= MIN)                                 \
+    _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = EXPR;
+  RESQ_STEP(2, v[i] + dpp<kDppXor1>(v[i]))
+  RESQ_STEP(4, v[i] + dpp<kDppXor2>(v[i]))
+  RESQ_STEP(8, v[i] + dpp<kDppHalfMirror>(v[i]))
+  RESQ_STEP(16, v[i] + dpp<kDppMirror>(v[i]))
+  RESQ_STEP(32, add_swapped<false>(v[i]))
+  RESQ_STEP(64, add_swapped<true>(v[i]))
+#undef RESQ_STEP
   if (L > 64) {
-    const int wave = threadIdx.x >> 6, waves = L >> 6;
+    const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) lds[i * kMaxWaves + wave] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      T t = lds[i * kMaxWaves];
-      for (int w = 1; w < waves; ++w) t += lds[i * kMaxWaves + w];
-      v[i] = t;
-    }
+    for (int i = 0; i < N; ++i) v[i] = T(0);
+    for (int w = 0; w < (L >> 6); w += 4)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const T* q = lds + i * kMaxWaves + w;
+        v[i] += (q[0] + q[1]) + (q[2] + q[3]);
+      }
   }
 }
 
@@ -52,87 +95,133 @@ __device__ __forceinline__ float rms_factor(double s, int64_t d, float eps) {
   return (float)(1.0 / sqrt(s / (double)d + (double)eps));
 }
 
-template <typename TH, typename TY, int C>
+// Where a lane's group c of a row lies.
+template <int E>
+struct Place {
+  int col, skip;  // first element; how many of its E elements another lane counts (E: all)
+};
+template <int E>
+__device__ __forceinline__ Place<E> place(int c, int L, int lane, int d) {
+  const int first = (c * L + lane) * E, col = min(first, d - E);
+  return {col, min(E, first - col)};
+}
+
+template <int E>
+__device__ __forceinline__ void load_gate(const void* gate, bool f32, int col, float g[E]) {
+  if (f32) load_n<E>(reinterpret_cast<const float*>(gate) + col, g);
+  else load_n<E>(reinterpret_cast<const uint16_t*>(gate) + col, g);
+}
+__device__ __forceinline__ float token_gate(const void* gate, bool f32, int64_t row) {
+  return f32 ? reinterpret_cast<const float*>(gate)[row] : bf16_value(reinterpret_cast<const uint16_t*>(gate)[row]);
+}
+
+// What the branch is scaled by along its columns: alpha gamma_post, times a channel's gate.
+template <int E>
+__device__ __forceinline__ void branch_gain(const uint16_t* gamma_post, const void* gate, int gate_mode, bool gate_f32,
+                                            float alpha, int col, float w[E]) {
+#pragma unroll
+  for (int i = 0; i < E; ++i) w[i] = alpha;
+  float g[E];
+  if (gamma_post) {
+    load_n<E>(gamma_post + col, g);
+#pragma unroll
+    for (int i = 0; i < E; ++i) w[i] *= g[i];
+  }
+  if (gate_mode == kGateChannel) {
+    load_gate<E>(gate, gate_f32, col, g);
+#pragma unroll
+    for (int i = 0; i < E; ++i) w[i] *= g[i];
+  }
+}
+
+// Row and lane of a thread.  WAVES: the row's lanes are whole waves, so the row is one per wave.
+template <bool WAVES>
+__device__ __forceinline__ int row_in_block(int L) {
+  const int r = threadIdx.x / L;
+  return WAVES ? __builtin_amdgcn_readfirstlane(r) : r;
+}
+
+template <typename TH, typename TY, int E, int C, bool WAVES>
 __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd p, int L) {
   __shared__ double lds[2][kMaxWaves];
-  const int lane = threadIdx.x % L;
-  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / L) + threadIdx.x / L;
-  const bool in = row < p.m;
-  const TH* h = reinterpret_cast<const TH*>(p.h) + row * p.ldh;
-  const TY* y = reinterpret_cast<const TY*>(p.y) + row * p.ldy;
-  float v[C][8], t[C][8];
-  int64_t col[C];
-  int n[C];
+  if (WAVES && L > 64) {  // whole waves in use write theirs; the gaps of the last four stay zero
+    if (threadIdx.x < 2 * kMaxWaves) lds[0][threadIdx.x] = 0.0;
+    __syncthreads();
+  }
+  const int sub = row_in_block<WAVES>(L), lane = threadIdx.x - sub * L, d = (int)p.d;
+  const int64_t row0 = (int64_t)blockIdx.x * (blockDim.x / L) + sub, row = min(row0, p.m - 1);
+  const bool in = row0 < p.m;
+  const bool first = in && lane == 0, post = p.gamma_post != nullptr, pre = p.gamma_pre != nullptr;
+  Place<E> at[C];
+  Raw<TH, E> raw_h[C];
+  Raw<TY, E> raw_y[C];
+  float v[C][E], t[C][E];
+  // every load first: gains and gates arrive under the statistics
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    col[c] = ((int64_t)c * L + lane) * 8;
-    n[c] = in ? (int)max((int64_t)0, min((int64_t)8, p.d - col[c])) : 0;
+    at[c] = place<E>(c, L, lane, d);
+    load_raw(reinterpret_cast<const TH*>(p.h) + row * p.ldh + at[c].col, raw_h[c]);
   }
+  if (p.y)
 #pragma unroll
-  for (int c = 0; c < C; ++c) load_upto8(h + col[c], n[c], 0.f, v[c]);
-  if (p.y) {
+    for (int c = 0; c < C; ++c) load_raw(reinterpret_cast<const TY*>(p.y) + row * p.ldy + at[c].col, raw_y[c]);
+  Raw<uint16_t, E> raw_pre[C];
+  if (pre)
 #pragma unroll
-    for (int c = 0; c < C; ++c) load_upto8(y + col[c], n[c], 0.f, t[c]);
-    if (p.gamma_post) {
-      double s[1] = {0.0};
+    for (int c = 0; c < C; ++c) load_raw(p.gamma_pre + at[c].col, raw_pre[c]);
+  float w[C][E];
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = fma((double)t[c][i], (double)t[c][i], s[0]);
-      row_sum<1>(s, L, lds[0]);
-      const float r = rms_factor(s[0], p.d, p.eps);
-      if (p.rstd && in && lane == 0) p.rstd[row] = r;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float g[8];
-        load_upto8(p.gamma_post + col[c], n[c], 0.f, g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[c][i] = t[c][i] * r * g[i];
-      }
-    }
-    float a = p.alpha;
-    if (p.gate_mode == kGateToken && in)
-      a *= p.gate_f32 ? reinterpret_cast<const float*>(p.gate)[row]
-                      : bf16_value(reinterpret_cast<const uint16_t*>(p.gate)[row]);
-    TH* ho = reinterpret_cast<TH*>(p.h_out) + row * p.ldho;
+  for (int c = 0; c < C; ++c) branch_gain<E>(p.gamma_post, p.gate, p.gate_mode, p.gate_f32, p.alpha, at[c].col, w[c]);
+  const float gt = p.gate_mode == kGateToken ? token_gate(p.gate, p.gate_f32, row) : 1.f;
+  auto factor = [&](const float (&z)[C][E], double* scratch) {
+    double s[1] = {0.0};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      if (p.gate_mode == kGateChannel) {
-        float g[8];
-        if (p.gate_f32) load_upto8(reinterpret_cast<const float*>(p.gate) + col[c], n[c], 0.f, g);
-        else load_upto8(reinterpret_cast<const uint16_t*>(p.gate) + col[c], n[c], 0.f, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[c][i] *= g[i];
-      }
+      for (int i = 0; i < E; ++i) s[0] = fma((double)z[c][i], i >= at[c].skip ? (double)z[c][i] : 0.0, s[0]);
+    }
+    row_sum<1>(s, L, scratch);
+    return rms_factor(s[0], p.d, p.eps);
+  };
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[c][i] = fmaf(a, t[c][i], v[c][i]);
+  for (int c = 0; c < C; ++c) unpack(raw_h[c], v[c]);
+  if (p.y) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) unpack(raw_y[c], t[c]);
+    float r = gt;
+    if (post) {
+      const float f = factor(t, lds[0]);
+      if (p.rstd && first) p.rstd[row] = f;
+      r *= f;
+    } else {
+      if (p.rstd && first) p.rstd[row] = 0.f;
+      if (L > 64 && d % E != 0) __syncthreads();  // every load before the first store of h'
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        v[c][i] = fmaf(t[c][i] * r, w[c][i], v[c][i]);
         if constexpr (sizeof(TH) == 2) v[c][i] = bf16_value(bf16_bits(v[c][i]));
       }
-      store_upto8(ho + col[c], n[c], v[c]);
+      if (in && at[c].skip < E) store_n<E>(reinterpret_cast<TH*>(p.h_out) + row * p.ldho + at[c].col, v[c]);
     }
+  } else if (p.rstd && first) {
+    p.rstd[row] = 0.f;
   }
-  if (p.rstd && in && lane == 0 && !(p.y && p.gamma_post)) p.rstd[row] = 0.f;
-  if (!p.gamma_pre) {
-    if (p.rstd && in && lane == 0) p.rstd[p.m + row] = 0.f;
+  if (!pre) {
+    if (p.rstd && first) p.rstd[p.m + row] = 0.f;
     return;
   }
-  double s[1] = {0.0};
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s[0] = fma((double)v[c][i], (double)v[c][i], s[0]);
-  row_sum<1>(s, L, lds[1]);
-  const float r = rms_factor(s[0], p.d, p.eps);
-  if (p.rstd && in && lane == 0) p.rstd[p.m + row] = r;
-  uint16_t* x = p.x + row * p.ldx;
+  const float r = factor(v, lds[1]);
+  if (p.rstd && first) p.rstd[p.m + row] = r;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    float g[8];
-    load_upto8(p.gamma_pre + col[c], n[c], 0.f, g);
+    float g[E];
+    unpack(raw_pre[c], g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = v[c][i] * r * g[i];
-    store_upto8(x + col[c], n[c], g);
+    for (int i = 0; i < E; ++i) g[i] = v[c][i] * r * g[i];
+    if (in && at[c].skip < E) store_n<E>(p.x + row * p.ldx + at[c].col, g);
   }
 }
 
@@ -142,171 +231,262 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd p, int L) {
 //   dy = r_y (dt gamma_post - yn k),  k = mean(dt gamma_post yn)   (dy = dt without the norm)
 //   dg = sum of alpha e t over the axis that g is broadcast along
 //   dgamma_pre = sum over rows of dx hn,  dgamma_post = sum over rows of dt yn
-// With w = alpha gamma_post yn (times g of the channel) the second mean follows from sums that
-// need no c: sum(w e) = sum(w (dh' + r_h dx gamma_pre)) - r_h c sum(w hn), so one reduction per
-// row gives c, k and a token's dg.
-// A workgroup walks over rows and keeps the column sums in registers; each of its row groups
-// writes one row of partial sums, which norm_bwd_sum_kernel adds in a fixed order.
-template <typename TH, typename TY, typename TX, int C>
+// A channel's gate and gain are constant along its column, so one column sum, B = sum of e yn
+// (times a token's g), gives both: dgamma_post = alpha g B, dg = alpha gamma_post B.
+// With w = alpha gamma_post (times g of the channel) the second mean follows from sums that need no
+// c: sum(w yn e) = sum(w yn (dh' + r_h dx gamma_pre)) - r_h c sum(w yn hn), so one reduction per row
+// gives c, k and a token's dg.
+// A workgroup walks over rows and keeps the column sums in registers; writes one
+// row of partial sums, which norm_bwd_sum_kernel adds in a fixed order.
+template <typename TH, typename TY, typename TX, int E, int C, bool WAVES>
 __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
   __shared__ float lds[2][3 * kMaxWaves];
-  const int lane = threadIdx.x % L, groups = blockDim.x / L;
-  const int64_t group = (int64_t)blockIdx.x * groups + threadIdx.x / L, n_groups = (int64_t)gridDim.x * groups;
-  const bool pre = p.gamma_pre != nullptr, post = p.gamma_post != nullptr;
-  const bool need_y = p.y != nullptr;
-  int64_t col[C];
-  int nc[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    col[c] = ((int64_t)c * L + lane) * 8;
-    nc[c] = (int)max((int64_t)0, min((int64_t)8, p.d - col[c]));
+  if (WAVES && L > 64) {
+    if (threadIdx.x < 6 * kMaxWaves) lds[0][threadIdx.x] = 0.f;
+    __syncthreads();
   }
-  float s_pre[C][8] = {}, s_post[C][8] = {}, s_gate[C][8] = {};
+  const int sub = row_in_block<WAVES>(L), lane = threadIdx.x - sub * L, d = (int)p.d, groups = blockDim.x / L;
+  const int64_t group = (int64_t)blockIdx.x * groups + sub, n_groups = (int64_t)gridDim.x * groups;
+  const bool pre = p.gamma_pre != nullptr, post = p.gamma_post != nullptr, need_y = p.y != nullptr;
+  Place<E> at[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) at[c] = place<E>(c, L, lane, d);
+  float s_pre[C][E] = {}, s_branch[C][E] = {};
+  float hn[E], dx[E], e[E], yn[E];  // of one group; e starts as dh', yn as y
+  float kept[E];  // C > 1: dh' of a group that was moved back (its neighbour may store to it)
+  Raw<TH, E> raw_h, raw_e;
+  Raw<TX, E> raw_x;
+  Raw<TY, E> raw_y;
+  Raw<uint16_t, E> raw_pre;
+  float w[E];
+  auto gains = [&](int col) {
+    if (pre) load_raw(p.gamma_pre + col, raw_pre);
+    branch_gain<E>(p.gamma_post, p.gate, p.gate_mode, p.gate_f32, p.alpha, col, w);
+  };
+  auto fetch = [&](int64_t row, int col) {
+    if (pre) {
+      load_raw(reinterpret_cast<const TH*>(p.h) + row * p.ldh + col, raw_h);
+      load_raw(reinterpret_cast<const TX*>(p.dx) + row * p.lddx + col, raw_x);
+    }
+    if (p.dho) load_raw(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col, raw_e);
+    if (need_y) load_raw(reinterpret_cast<const TY*>(p.y) + row * p.ldy + col, raw_y);
+  };
+  auto take = [&](float rh, float ry) {
+    if (pre) {
+      unpack(raw_h, hn);
+      unpack(raw_x, dx);
+#pragma unroll
+      for (int i = 0; i < E; ++i) hn[i] *= rh;
+    }
+    if (p.dho) unpack(raw_e, e);
+    else
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = 0.f;
+    if (need_y) {
+      unpack(raw_y, yn);
+#pragma unroll
+      for (int i = 0; i < E; ++i) yn[i] *= ry;
+    }
+  };
   const int64_t trips = (p.m + n_groups - 1) / n_groups;
+  // One group per lane: the gains stay in registers, and the next row's loads run under this row's
+  // sums and stores.  (A load inside the loop would have to wait for them: loads return in order.)
+  float next_rh = 0.f, next_ry = 1.f, next_gt = 1.f;
+  auto fetch_factors = [&](int64_t row) {
+    if (pre) next_rh = p.rstd[p.m + row];
+    if (post) next_ry = p.rstd[row];
+    if (p.gate_mode == kGateToken) next_gt = token_gate(p.gate, p.gate_f32, row);
+  };
+  fetch_factors(min(group, p.m - 1));
+  if constexpr (C == 1) {
+    gains(at[0].col);
+    fetch(min(group, p.m - 1), at[0].col);
+  }
   for (int64_t k = 0; k < trips; ++k) {  // the same count for every lane: row_sum has a barrier
-    const int64_t row = group + k * n_groups;
+    const int64_t row = group + k * n_groups, next = min(row + n_groups, p.m - 1);
     const bool in = row < p.m;
-    float h[C][8], u[C][8], e[C][8], yn[C][8];
-    const float rh = pre && in ? p.rstd[p.m + row] : 0.f, ry = post && in ? p.rstd[row] : 1.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int n = in ? nc[c] : 0;
-      if (pre) {
-        load_upto8(reinterpret_cast<const TH*>(p.h) + row * p.ldh + col[c], n, 0.f, h[c]);
-        load_upto8(reinterpret_cast<const TX*>(p.dx) + row * p.lddx + col[c], n, 0.f, u[c]);
-      }
-      if (p.dho) load_upto8(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col[c], n, 0.f, e[c]);
-      else
-        for (int i = 0; i < 8; ++i) e[c][i] = 0.f;
-      if (need_y) load_upto8(reinterpret_cast<const TY*>(p.y) + row * p.ldy + col[c], n, 0.f, yn[c]);
-    }
-    float gt = 1.f;
-    if (p.gate_mode == kGateToken && in)
-      gt = p.gate_f32 ? reinterpret_cast<const float*>(p.gate)[row]
-                      : bf16_value(reinterpret_cast<const uint16_t*>(p.gate)[row]);
+    const float rh = next_rh, ry = next_ry, gt = next_gt;
     float s[3] = {0.f, 0.f, 0.f};
+    if (in) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (pre) {
-        float g[8];
-        load_upto8(p.gamma_pre + col[c], nc[c], 0.f, g);
+      for (int c = 0; c < C; ++c) {
+        const int col = at[c].col;
+        if constexpr (C > 1) {
+          __builtin_amdgcn_sched_barrier(0);  // one group's loads at a time: two do not fit the registers
+          gains(col);
+          fetch(row, col);
+        }
+        take(rh, ry);
+        if constexpr (C == 1) fetch(next, col);
+        if constexpr (C > 1)
+          if (at[c].skip > 0)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          h[c][i] *= rh;
-          s_pre[c][i] = fmaf(u[c][i], h[c][i], s_pre[c][i]);
-          u[c][i] *= g[i];
-          s[0] = fmaf(u[c][i], h[c][i], s[0]);
-          e[c][i] = fmaf(rh, u[c][i], e[c][i]);
-        }
-      }
-      if (need_y) {
-        float gp[8], gc[8];
-        if (post) load_upto8(p.gamma_post + col[c], nc[c], 0.f, gp);
-        if (p.gate_mode == kGateChannel) {
-          if (p.gate_f32) load_upto8(reinterpret_cast<const float*>(p.gate) + col[c], nc[c], 0.f, gc);
-          else load_upto8(reinterpret_cast<const uint16_t*>(p.gate) + col[c], nc[c], 0.f, gc);
-        }
+            for (int i = 0; i < E; ++i) kept[i] = e[i];
+        if (pre) {
+          float g[E];
+          unpack(raw_pre, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          yn[c][i] *= ry;
-          float w = p.alpha * yn[c][i];
-          if (post) w *= gp[i];
-          if (p.gate_mode == kGateChannel) w *= gc[i];
-          s[1] = fmaf(w, e[c][i], s[1]);
-          if (pre) s[2] = fmaf(w, h[c][i], s[2]);
+          for (int i = 0; i < E; ++i) {
+            if constexpr (C == 1) s_pre[c][i] = fmaf(dx[i], hn[i], s_pre[c][i]);
+            const float u = dx[i] * g[i];
+            s[0] = fmaf(u, i >= at[c].skip ? hn[i] : 0.f, s[0]);
+            e[i] = fmaf(rh, u, e[i]);
+          }
         }
+        if (need_y)
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const float wy = i >= at[c].skip ? w[i] * yn[i] : 0.f;
+            s[1] = fmaf(wy, e[i], s[1]);
+            if (pre) s[2] = fmaf(wy, hn[i], s[2]);
+          }
       }
     }
+    fetch_factors(next);
     row_sum<3>(s, L, lds[k & 1]);
-    const float rc = rh * (s[0] / (float)p.d);
-    const float we = s[1] - rc * s[2];
-    if (p.gate_mode == kGateToken && p.dgate && in && lane == 0) p.dgate[row] = we;
-    const float km = we * gt / (float)p.d, a = p.alpha * gt;
+    if (!in) continue;
+    const float rc = rh * (s[0] / (float)d);
+    const float we = s[1] - rc * s[2];  // sum(w yn e)
+    if (p.gate_mode == kGateToken && p.dgate && lane == 0) p.dgate[row] = we;
+    const float km = we * gt / (float)d;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int n = in ? nc[c] : 0;
+      const int col = at[c].col;
+      const bool mine = at[c].skip < E;
+      if constexpr (C > 1) {
+        __builtin_amdgcn_sched_barrier(0);  // two groups do not stay in registers beside the column sums
+        gains(col);
+        fetch(row, col);
+        take(rh, ry);
+        if (at[c].skip > 0)
+#pragma unroll
+          for (int i = 0; i < E; ++i) e[i] = kept[i];
+        if (pre) {
+          float g[E];
+          unpack(raw_pre, g);
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            s_pre[c][i] = fmaf(dx[i], hn[i], s_pre[c][i]);
+            e[i] = fmaf(rh, dx[i] * g[i], e[i]);
+          }
+        }
+      }
       if (pre)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[c][i] = fmaf(-rc, h[c][i], e[c][i]);
-      if (p.dh) store_upto8(reinterpret_cast<TH*>(p.dh) + row * p.lddh + col[c], n, e[c]);
-      if (!need_y && !p.dy) continue;
-      float gp[8], gc[8];
-      if (post) load_upto8(p.gamma_post + col[c], nc[c], 0.f, gp);
-      if (p.gate_mode == kGateChannel) {
-        if (p.gate_f32) load_upto8(reinterpret_cast<const float*>(p.gate) + col[c], nc[c], 0.f, gc);
-        else load_upto8(reinterpret_cast<const uint16_t*>(p.gate) + col[c], nc[c], 0.f, gc);
-      }
+        for (int i = 0; i < E; ++i) e[i] = fmaf(-rc, hn[i], e[i]);
+      if (p.dh && mine) {
+        TH* dst = reinterpret_cast<TH*>(p.dh) + row * p.lddh + col;
+        if (C > 1 && at[c].skip > 0) {  // its neighbour may still have to read dh' there
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float dt = a * e[c][i];
-        if (p.gate_mode == kGateChannel) {
-          if (p.part_gate) s_gate[c][i] = fmaf(dt * (post ? gp[i] : 1.f), yn[c][i], s_gate[c][i]);
-          dt *= gc[i];
+          for (int i = 0; i < E; ++i)
+            if (i >= at[c].skip) store1(dst + i, e[i]);
+        } else {
+          store_n<E>(dst, e);
         }
-        if (post) {
-          s_post[c][i] = fmaf(dt, yn[c][i], s_post[c][i]);
-          dt = ry * (dt * gp[i] - yn[c][i] * km);
-        }
-        e[c][i] = dt;
       }
-      if (p.dy) {
-        if (p.dy_f32) store_upto8(reinterpret_cast<float*>(p.dy) + row * p.lddy + col[c], n, e[c]);
-        else store_upto8(reinterpret_cast<uint16_t*>(p.dy) + row * p.lddy + col[c], n, e[c]);
+      if (need_y)
+#pragma unroll
+        for (int i = 0; i < E; ++i) s_branch[c][i] = fmaf(gt * e[i], yn[i], s_branch[c][i]);
+      if (p.dy && mine) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          e[i] *= gt * w[i];
+          if (post) e[i] = ry * (e[i] - yn[i] * km);
+        }
+        if (p.dy_f32) store_n<E>(reinterpret_cast<float*>(p.dy) + row * p.lddy + col, e);
+        else store_n<E>(reinterpret_cast<uint16_t*>(p.dy) + row * p.lddy + col, e);
       }
     }
   }
-  // partial sums: [vector][group][d]
+  // The workgroup's partial sums, [gridDim.x][d] each: row groups of one wave are added by lane
+  // exchange, those of its four waves through LDS in wave order.
+  auto put = [&](float* part, float (&v)[C][E]) {
+    if (part == nullptr) return;  // uniform
+    if (L <= 64) {
+      __shared__ float rows[4][64 * E];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if (p.part_pre) store_upto8(p.part_pre + group * p.d + col[c], nc[c], s_pre[c]);
-    if (p.part_post) store_upto8(p.part_post + group * p.d + col[c], nc[c], s_post[c]);
-    if (p.part_gate) store_upto8(p.part_gate + group * p.d + col[c], nc[c], s_gate[c]);
-  }
+      for (int i = 0; i < E; ++i) {
+        for (int o = L; o < 64; o <<= 1) v[0][i] += __shfl_xor(v[0][i], o, 64);
+        rows[threadIdx.x >> 6][(threadIdx.x & 63) * E + i] = v[0][i];
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < L)
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          v[0][i] = (rows[0][threadIdx.x * E + i] + rows[1][threadIdx.x * E + i]) +
+                    (rows[2][threadIdx.x * E + i] + rows[3][threadIdx.x * E + i]);
+      __syncthreads();
+      if ((int)threadIdx.x >= L) return;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (at[c].skip < E) store_n<E>(part + (int64_t)blockIdx.x * p.d + at[c].col, v[c]);
+  };
+  put(p.part_pre, s_pre);
+  put(p.part_branch, s_branch);
 }
 
 struct ColumnSums {
-  const float* part[3];
-  float* out[3];
+  const float* part[2];  // of dx hn and of the branch (B above), [n_parts][d]; null: not wanted
+  float *dgamma_pre, *dgamma_post, *dgate;
+  const uint16_t* gamma_post;
+  const void* gate;  // per channel, or null
+  bool gate_f32;
+  float alpha;
 };
 
-// out[j] = sum over the n_groups partial rows of column j, in float64: a workgroup takes 64
-// columns, its 16 waves every 16th row, and the waves' sums are added in order.
-__global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(ColumnSums q, int64_t n_groups, int64_t d) {
-  __shared__ double lds[16][64];
-  const float* part = q.part[blockIdx.y];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
+// The n_parts partial rows of column j added in float64: a workgroup takes 32 columns (a row's
+// 128-byte line), its 32 slices every 32nd row, and the slices are added in a fixed order.
+__global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(ColumnSums q, int64_t n_parts, int64_t d) {
+  __shared__ double lds[32][32];
+  const bool branch = q.part[0] == nullptr || blockIdx.y == 1;
+  const float* part = q.part[branch];
+  const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t j = (int64_t)blockIdx.x * 32 + lane;
   double s = 0.0;
   if (j < d)
-#pragma unroll 4
-    for (int64_t g = wave; g < n_groups; g += 16) s += (double)part[g * d + j];
-  lds[wave][lane] = s;
+#pragma unroll 8
+    for (int64_t g = slice; g < n_parts; g += 32) s += (double)part[g * d + j];
+  lds[slice][lane] = s;
   __syncthreads();
-  if (wave == 0 && j < d) {
-    for (int w = 1; w < 16; ++w) s += lds[w][lane];
-    q.out[blockIdx.y][j] = (float)s;
+  if (slice < 4)
+    for (int w = 1; w < 8; ++w) s += lds[slice + 4 * w][lane];
+  __syncthreads();
+  if (slice < 4) lds[slice][lane] = s;
+  __syncthreads();
+  if (slice != 0 || j >= d) return;
+  s = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+  if (!branch) {
+    q.dgamma_pre[j] = (float)s;
+    return;
   }
+  s *= (double)q.alpha;
+  if (q.dgamma_post) {
+    double g = 1.0;
+    if (q.gate) g = q.gate_f32 ? reinterpret_cast<const float*>(q.gate)[j] : bf16_value(reinterpret_cast<const uint16_t*>(q.gate)[j]);
+    q.dgamma_post[j] = (float)(s * g);
+  }
+  if (q.dgate) q.dgate[j] = (float)(q.gamma_post ? s * (double)bf16_value(q.gamma_post[j]) : s);
 }
 
 struct RowLanes {
-  int L, threads, C;
+  int L, threads;
+  bool one, wide;  // rows shorter than 8: E = 1; longer than 8192: sixteen elements per lane
 };
 
-// Lanes per row and groups of eight per lane: up to 64 lanes a power of two, several rows to a
-// workgroup of 256; beyond, whole waves.
+// Lanes per row: up to 32 lanes a power of two, several rows to a wave; beyond, whole waves.
 RowLanes row_lanes(int64_t d) {
-  const int64_t g = (d + 7) / 8;
   RowLanes r{};
-  r.C = g <= 256 ? 1 : 2;
-  const int64_t lanes = (g + r.C - 1) / r.C;
-  if (lanes <= 64) {
+  r.one = d < 8;
+  r.wide = d > 8192;
+  const int64_t lanes = r.one ? d : r.wide ? (d + 15) / 16 : (d + 7) / 8;
+  if (lanes <= 32) {
     r.L = 1;
     while (r.L < lanes) r.L *= 2;
-    r.threads = 256;
   } else {
     r.L = (int)((lanes + 63) / 64 * 64);
-    r.threads = r.L;
   }
+  r.threads = r.L <= 64 ? 256 : r.L;
   return r;
 }
 
@@ -320,16 +500,21 @@ int64_t bwd_workgroups(int64_t m, int64_t d) {
 
 size_t norm_bwd_ws_bytes(int64_t m, int64_t d) {
   if (m <= 0 || d <= 0 || d > kNormMaxD) return 0;
-  const RowLanes r = row_lanes(d);
-  return (size_t)bwd_workgroups(m, d) * (r.threads / r.L) * d * 3 * sizeof(float);
+  return (size_t)bwd_workgroups(m, d) * d * 2 * sizeof(float);
 }
 
 void launch_norm_fwd(const NormFwd& p, bool h_f32, bool y_f32, hipStream_t s) {
   const RowLanes r = row_lanes(p.d);
   const int64_t rows = r.threads / r.L;
   const dim3 grid((unsigned)((p.m + rows - 1) / rows)), block(r.threads);
-#define RESQ_NF(H, Y, C) launch_timed(norm_fwd_kernel<H, Y, C>, grid, block, 0u, s, p, r.L)
-#define RESQ_NF2(H, Y) do { if (r.C == 1) RESQ_NF(H, Y, 1); else RESQ_NF(H, Y, 2); } while (0)
+#define RESQ_NF(H, Y, E, C, W) launch_timed(norm_fwd_kernel<H, Y, E, C, W>, grid, block, 0u, s, p, r.L)
+#define RESQ_NF2(H, Y)                         \
+  do {                                         \
+    if (r.one) RESQ_NF(H, Y, 1, 1, false);     \
+    else if (r.L < 64) RESQ_NF(H, Y, 8, 1, false); \
+    else if (!r.wide) RESQ_NF(H, Y, 8, 1, true);   \
+    else RESQ_NF(H, Y, 8, 2, true);            \
+  } while (0)
   if (h_f32) { if (y_f32) RESQ_NF2(float, float); else RESQ_NF2(float, uint16_t); }
   else { if (y_f32) RESQ_NF2(uint16_t, float); else RESQ_NF2(uint16_t, uint16_t); }
 #undef RESQ_NF2
@@ -339,24 +524,28 @@ void launch_norm_fwd(const NormFwd& p, bool h_f32, bool y_f32, hipStream_t s) {
 void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgamma_post, float* dgamma_pre,
                      float* workspace, hipStream_t s) {
   const RowLanes r = row_lanes(p.d);
-  const int64_t wgs = bwd_workgroups(p.m, p.d), n_groups = wgs * (r.threads / r.L);
+  const int64_t wgs = bwd_workgroups(p.m, p.d);
+  const bool channel = p.gate_mode == kGateChannel;
   ColumnSums q{};
-  int nv = 0;
-  float* next = workspace;
-  auto sums = [&](float* out) -> float* {
-    if (!out) return nullptr;
-    float* part = next;
-    next += n_groups * p.d;
-    q.part[nv] = part;
-    q.out[nv++] = out;
-    return part;
-  };
-  p.part_pre = sums(dgamma_pre);
-  p.part_post = sums(dgamma_post);
-  p.part_gate = sums(p.gate_mode == kGateChannel ? p.dgate : nullptr);
+  q.dgamma_pre = dgamma_pre;
+  q.dgamma_post = dgamma_post;
+  q.dgate = channel ? p.dgate : nullptr;
+  q.gamma_post = p.gamma_post;
+  q.gate = channel ? p.gate : nullptr;
+  q.gate_f32 = p.gate_f32;
+  q.alpha = p.alpha;
+  if (dgamma_pre) q.part[0] = p.part_pre = workspace;
+  if (q.dgamma_post || q.dgate) q.part[1] = p.part_branch = workspace + wgs * p.d;
+  const int nv = (q.part[0] ? 1 : 0) + (q.part[1] ? 1 : 0);
   const dim3 grid((unsigned)wgs), block(r.threads);
-#define RESQ_NB(H, Y, X, C) launch_timed(norm_bwd_kernel<H, Y, X, C>, grid, block, 0u, s, p, r.L)
-#define RESQ_NB2(H, Y, X) do { if (r.C == 1) RESQ_NB(H, Y, X, 1); else RESQ_NB(H, Y, X, 2); } while (0)
+#define RESQ_NB(H, Y, X, E, C, W) launch_timed(norm_bwd_kernel<H, Y, X, E, C, W>, grid, block, 0u, s, p, r.L)
+#define RESQ_NB2(H, Y, X)                             \
+  do {                                                \
+    if (r.one) RESQ_NB(H, Y, X, 1, 1, false);         \
+    else if (r.L < 64) RESQ_NB(H, Y, X, 8, 1, false); \
+    else if (!r.wide) RESQ_NB(H, Y, X, 8, 1, true);   \
+    else RESQ_NB(H, Y, X, 4, 4, true);                \
+  } while (0)
 #define RESQ_NB3(H, Y) do { if (dx_f32) RESQ_NB2(H, Y, float); else RESQ_NB2(H, Y, uint16_t); } while (0)
   if (h_f32) { if (y_f32) RESQ_NB3(float, float); else RESQ_NB3(float, uint16_t); }
   else { if (y_f32) RESQ_NB3(uint16_t, float); else RESQ_NB3(uint16_t, uint16_t); }
@@ -364,8 +553,7 @@ void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgam
 #undef RESQ_NB2
 #undef RESQ_NB
   if (nv > 0)
-    launch_timed(norm_bwd_sum_kernel, dim3((unsigned)((p.d + 63) / 64), (unsigned)nv), dim3(1024), 0u, s, q, n_groups,
-                 p.d);
+    launch_timed(norm_bwd_sum_kernel, dim3((unsigned)((p.d + 31) / 32), (unsigned)nv), dim3(1024), 0u, s, q, wgs, p.d);
 }
 
 }  // namespace resq

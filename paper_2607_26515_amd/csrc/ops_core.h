@@ -11,10 +11,12 @@
 namespace resq {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 struct __attribute__((packed, aligned(2))) Bf16x8 { u32x4 v; };
+struct __attribute__((packed, aligned(2))) Bf16x4 { u32x2 v; };
 struct __attribute__((packed, aligned(4))) F32x4 { f32x4 v; };
 
 __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
@@ -29,19 +31,6 @@ __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = bf16_bits(v); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 
-__device__ __forceinline__ void load8(const uint16_t* p, float v[8]) {
-  const u32x4 u = reinterpret_cast<const Bf16x8*>(p)->v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(u[i] << 16);
-    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ void load8(const float* p, float v[8]) {
-  const f32x4 a = reinterpret_cast<const F32x4*>(p)[0].v, b = reinterpret_cast<const F32x4*>(p)[1].v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-}
 __device__ __forceinline__ void store8(uint16_t* p, const float v[8]) {
   u32x4 u;
 #pragma unroll
@@ -54,6 +43,100 @@ __device__ __forceinline__ void store8(float* p, const float v[8]) {
   for (int i = 0; i < 4; ++i) { a[i] = v[i]; b[i] = v[4 + i]; }
   reinterpret_cast<F32x4*>(p)[0].v = a;
   reinterpret_cast<F32x4*>(p)[1].v = b;
+}
+
+// E consecutive elements as loaded, to be taken apart later (a load in flight holds no more registers
+// than its bytes).
+template <typename T, int E>
+struct Raw {
+  T v[E];
+};
+template <>
+struct Raw<uint16_t, 8> {
+  u32x4 v;
+};
+template <>
+struct Raw<uint16_t, 4> {
+  u32x2 v;
+};
+template <>
+struct Raw<float, 4> {
+  f32x4 a;
+};
+template <>
+struct Raw<float, 8> {
+  f32x4 a, b;
+};
+template <typename T>
+__device__ __forceinline__ void load_raw(const T* p, Raw<T, 1>& r) { r.v[0] = *p; }
+__device__ __forceinline__ void load_raw(const uint16_t* p, Raw<uint16_t, 8>& r) {
+  r.v = reinterpret_cast<const Bf16x8*>(p)->v;
+}
+__device__ __forceinline__ void load_raw(const uint16_t* p, Raw<uint16_t, 4>& r) {
+  r.v = reinterpret_cast<const Bf16x4*>(p)->v;
+}
+__device__ __forceinline__ void load_raw(const float* p, Raw<float, 4>& r) {
+  r.a = reinterpret_cast<const F32x4*>(p)->v;
+}
+__device__ __forceinline__ void load_raw(const float* p, Raw<float, 8>& r) {
+  r.a = reinterpret_cast<const F32x4*>(p)[0].v;
+  r.b = reinterpret_cast<const F32x4*>(p)[1].v;
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw<T, 1>& r, float v[1]) { v[0] = load1(&r.v[0]); }
+__device__ __forceinline__ void unpack(const Raw<uint16_t, 8>& r, float v[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(r.v[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r.v[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Raw<uint16_t, 4>& r, float v[4]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] = __uint_as_float(r.v[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r.v[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Raw<float, 4>& r, float v[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = r.a[i];
+}
+__device__ __forceinline__ void unpack(const Raw<float, 8>& r, float v[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = r.a[i]; v[4 + i] = r.b[i]; }
+}
+
+__device__ __forceinline__ void load8(const uint16_t* p, float v[8]) {
+  Raw<uint16_t, 8> r;
+  load_raw(p, r);
+  unpack(r, v);
+}
+__device__ __forceinline__ void load8(const float* p, float v[8]) {
+  Raw<float, 8> r;
+  load_raw(p, r);
+  unpack(r, v);
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, const float v[4]) {
+  reinterpret_cast<Bf16x4*>(p)->v = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+}
+__device__ __forceinline__ void store4(float* p, const float v[4]) {
+  reinterpret_cast<F32x4*>(p)->v = f32x4{v[0], v[1], v[2], v[3]};
+}
+
+// E consecutive elements (E = 8, 4 or 1).
+template <int E, typename T>
+__device__ __forceinline__ void load_n(const T* p, float v[E]) {
+  Raw<T, E> r;
+  load_raw(p, r);
+  unpack(r, v);
+}
+template <int E, typename T>
+__device__ __forceinline__ void store_n(T* p, const float v[E]) {
+  if constexpr (E == 8) store8(p, v);
+  else if constexpr (E == 4) store4(p, v);
+  else store1(p, v[0]);
 }
 
 // Elements 0 .. n - 1 of eight (n <= 0: none), the others `fill`.
