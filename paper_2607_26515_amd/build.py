@@ -28,9 +28,9 @@ FLAGS = [
 ]
 
 
-# Per-source extra flags.  The GEMMs: MFMA results in VGPRs (the HiF4 fold reads them with
+# Per-source extra flags.  The GEMMs and matvec: MFMA results in VGPRs (the HiF4 fold reads them with
 # VALU instructions, which cannot read AGPRs).
-EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("gemm.hip", "gemm_hif4.hip", "gemm_stream.hip")}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("gemm.hip", "gemm_hif4.hip", "gemm_stream.hip", "matvec.hip")}
 
 
 def _compile(src: str) -> str:

@@ -16,7 +16,6 @@
 // order, across waves by the barrier of a row sum, or one of their own where there is no sum.
 #include <algorithm>
 
-#include "device_fp4.h"
 #include "kernels.h"
 #include "ops_core.h"
 #include "profiler.h"
@@ -25,33 +24,6 @@ namespace resq {
 namespace {
 
 constexpr int kMaxWaves = 16;
-
-// A value from another lane of the same 16 (DPP; both halves of a double), and the sum with the
-// lanes 16 or 32 away (gfx950's half swaps).
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) { return __uint_as_float(dpp_u32<CTRL>(__float_as_uint(v))); }
-template <int CTRL>
-__device__ __forceinline__ double dpp(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  return __builtin_bit_cast(double, ((uint64_t)dpp_u32<CTRL>((uint32_t)(u >> 32)) << 32) | dpp_u32<CTRL>((uint32_t)u));
-}
-template <bool HALF>
-__device__ __forceinline__ u32x2 swap_rows(uint32_t v) {
-  if constexpr (HALF) return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
-  else return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
-}
-template <bool HALF>
-__device__ __forceinline__ float add_swapped(float v) {
-  const u32x2 r = swap_rows<HALF>(__float_as_uint(v));
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-template <bool HALF>
-__device__ __forceinline__ double add_swapped(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const u32x2 lo = swap_rows<HALF>((uint32_t)u), hi = swap_rows<HALF>((uint32_t)(u >> 32));
-  return __builtin_bit_cast(double, ((uint64_t)hi[0] << 32) | lo[0]) +
-         __builtin_bit_cast(double, ((uint64_t)hi[1] << 32) | lo[1]);
-}
 
 // Sum of N values per lane over the L lanes of a row (L a power of two up to 32, or a multiple of
 // 64: then, past 64, the whole workgroup is one row).  Every lane gets the sum; the order is fixed.

@@ -1,4 +1,5 @@
-// Loads, stores and sums shared by the row kernels (norm.hip, logprob.hip).
+// Loads, stores and sums shared by the row kernels and the few-token products (norm.hip,
+// logprob.hip, matvec.hip).
 //
 // Rows may start at any element: eight elements move in one or two 16-byte accesses with the
 // element's own alignment, which gfx950's memory system takes for global memory at any address
@@ -7,6 +8,8 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "device_fp4.h"
 
 namespace resq {
 
@@ -158,6 +161,34 @@ __device__ __forceinline__ void store_upto8(T* p, int n, const float v[8]) {
     for (int i = 0; i < 8; ++i)
       if (i < n) store1(p + i, v[i]);
   }
+}
+
+// A value from another lane of the same 16 (DPP; both halves of a double), and the sum with the
+// lanes 16 or 32 away (gfx950's half swaps).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __uint_as_float(dpp_u32<CTRL>(__float_as_uint(v))); }
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, ((uint64_t)dpp_u32<CTRL>((uint32_t)(u >> 32)) << 32) | dpp_u32<CTRL>((uint32_t)u));
+}
+constexpr int kDppRor4 = 0x124, kDppRor8 = 0x128;  // lane i of 16 <- lane i - 4, i - 8 (mod 16)
+template <bool HALF>
+__device__ __forceinline__ u32x2 swap_rows(uint32_t v) {
+  if constexpr (HALF) return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+  else return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+}
+template <bool HALF>
+__device__ __forceinline__ float add_swapped(float v) {
+  const u32x2 r = swap_rows<HALF>(__float_as_uint(v));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <bool HALF>
+__device__ __forceinline__ double add_swapped(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const u32x2 lo = swap_rows<HALF>((uint32_t)u), hi = swap_rows<HALF>((uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, ((uint64_t)hi[0] << 32) | lo[0]) +
+         __builtin_bit_cast(double, ((uint64_t)hi[1] << 32) | lo[1]);
 }
 
 }  // namespace resq
