@@ -9,11 +9,17 @@
 // sum relative to it, and the largest group of eight it has seen.  Few rows are split over several
 // workgroups, whose partial results a second kernel joins.
 //
-// Top k (k <= 32): the k-th largest of the lanes' largest elements bounds the k-th largest element
-// of the row from below, and every element at or above that bound lies with one of the k lanes
-// whose own largest is.  So only those lanes' elements are looked at again.  Elements are ranked by
-// 64-bit keys (the value's order-preserving pattern, then the inverted index), so ties go to the
-// lowest index and the result does not depend on the order of work.
+// Exponentials are taken to base 2 relative to a reference r = fl(M c), c = log2(e) / T: the element's
+// exponent y = fma(x, c, -r) is one instruction with one rounding at any offset of the logits, and what
+// r is off from M c is put right at the end.  About seven instructions per element: the loop is bound
+// by HBM for float32 logits and about evenly by HBM and the vector units for bf16.
+//
+// Top k (k <= 32): every lane keeps the largest group of eight that it has seen, by its largest value.
+// Ranked by (value, first index), the k-th largest of these over 64 sets of eight lanes bounds the k-th
+// largest element of the row from below, and every element at or above the bound lies with a lane whose
+// own group is: about k lanes.  Only those lanes' elements are looked at again.  Elements are ranked by 64-bit keys (the value's
+// order-preserving pattern, then the inverted index): ties go to the lowest index and the result does
+// not depend on the order of work.
 #include <algorithm>
 
 #include "kernels.h"
@@ -25,7 +31,9 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kGroup = 8;                            // elements per load
-constexpr int64_t kStep = (int64_t)kThreads * kGroup;  // elements per trip of a workgroup
+constexpr int64_t kStep = (int64_t)kThreads * kGroup;  // elements that a workgroup's lanes load at once
+constexpr int kUnroll = 4;
+constexpr int64_t kTrip = kStep * kUnroll;
 
 // Descending order of values as ascending-free unsigned keys: larger value, then lower index.
 // -inf and NaN are no alternatives: key 0.
@@ -41,81 +49,102 @@ __device__ __forceinline__ float key_value(uint64_t k) {
   return __uint_as_float(o ^ ((uint32_t)((int32_t)~o >> 31) | 0x80000000u));
 }
 
-__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int o) {
-  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64), hi = (uint32_t)__shfl_xor((int)(v >> 32), o, 64);
-  return ((uint64_t)hi << 32) | lo;
-}
-
-// The wave's 64 keys in descending order by lane (bitonic sort).
-__device__ __forceinline__ uint64_t sort64(uint64_t v, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      const uint64_t o = shfl_xor_u64(v, j);
-      const bool keep_max = ((lane & j) == 0) == ((lane & k) == 0);
-      v = keep_max ? max(v, o) : min(v, o);
-    }
-  return v;
-}
-// Lanes 0..31 and, reversed, 32..63 hold descending lists: the 64 keys in descending order.
-__device__ __forceinline__ uint64_t merge64(uint64_t v, int lane) {
-#pragma unroll
-  for (int j = 32; j > 0; j >>= 1) {
-    const uint64_t o = shfl_xor_u64(v, j);
-    v = (lane & j) == 0 ? max(v, o) : min(v, o);
+// The 32 bits of lane ^ J.
+template <int J>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
+  if constexpr (J == 1) return dpp_u32<kDppXor1>(v);
+  else if constexpr (J == 2) return dpp_u32<kDppXor2>(v);
+  else if constexpr (J == 4) return dpp_u32<0x1B>(dpp_u32<kDppHalfMirror>(v));  // ^ 7, then ^ 3 (quad reversed)
+  else if constexpr (J == 8) return dpp_u32<kDppRor8>(v);
+  else if constexpr (J == 16) {
+    const u32x2 r = swap_rows<false>(v);
+    return (lane & 16) ? r[0] : r[1];
+  } else {
+    const u32x2 r = swap_rows<true>(v);
+    return (lane & 32) ? r[0] : r[1];
   }
-  return v;
+}
+template <int J>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int lane) {
+  return ((uint64_t)lane_xor<J>((uint32_t)(v >> 32), lane) << 32) | lane_xor<J>((uint32_t)v, lane);
+}
+// One step of a bitonic network: lanes J apart, the larger key to the lane with `up`.
+template <int J>
+__device__ __forceinline__ uint64_t exchange(uint64_t v, int lane, bool up) {
+  const uint64_t o = lane_xor<J>(v, lane);
+  return (v > o) == up ? v : o;
+}
+template <int K, int J>
+__device__ __forceinline__ uint64_t sort_steps(uint64_t v, int lane) {
+  v = exchange<J>(v, lane, ((lane & J) == 0) == ((lane & K) == 0));
+  if constexpr (J > 1) return sort_steps<K, J / 2>(v, lane);
+  else if constexpr (K < 64) return sort_steps<K * 2, K>(v, lane);
+  else return v;
+}
+// The wave's 64 keys in descending order by lane (a bitonic network on lane exchanges, no LDS).
+__device__ __forceinline__ uint64_t sort64(uint64_t v, int lane) { return sort_steps<2, 1>(v, lane); }
+// Lanes 0..31 and, reversed, 32..63 hold descending lists: the 64 keys in descending order.
+__device__ __forceinline__ uint64_t merge64(uint64_t v, int lane) { return sort_steps<64, 32>(v, lane); }
+// The list in lanes 0..31 reversed into lanes 32..63.
+__device__ __forceinline__ uint64_t reversed(uint64_t v, int lane) {
+  v = lane_xor<32>(v, lane);
+  v = lane_xor<16>(v, lane);
+  return ((uint64_t)dpp_u32<kDppMirror>((uint32_t)(v >> 32)) << 32) | dpp_u32<kDppMirror>((uint32_t)v);
 }
 // Takes 64 more keys into the descending list of 32 in lanes 0..31.
 __device__ __forceinline__ uint64_t take64(uint64_t list, uint64_t more, int lane) {
-  const uint64_t least = ((uint64_t)(uint32_t)__shfl((int)(list >> 32), 31, 64) << 32) |
-                         (uint32_t)__shfl((int)(uint32_t)list, 31, 64);
-  if (__ballot(more > least) == 0ull) return list;
   more = sort64(more, lane);
-  // the 32 largest of them, reversed, in lanes 32..63
-  const uint64_t rev = shfl_xor_u64(more, 63);
+  const uint64_t rev = reversed(more, lane);
   return merge64(lane < 32 ? list : rev, lane);
 }
 
-// Joins the waves' lists (lanes 0..31 of each) in wave 0.  Every wave must call it.
-__device__ __forceinline__ uint64_t join_waves(uint64_t list, uint64_t (*lds)[32], int lane, int wave) {
+// Joins the waves' descending lists (lanes 0..31 of each) in wave 0, halving the waves.  Every wave
+// must call it.
+__device__ __forceinline__ uint64_t join_lists(uint64_t list, uint64_t (*lists)[32], int tid) {
+  const int lane = tid & 63, wave = tid >> 6;
   for (int half = kWaves / 2; half > 0; half >>= 1) {
     __syncthreads();
-    if (wave >= half && wave < 2 * half && lane < 32) lds[wave - half][lane] = list;
+    if (wave >= half && wave < 2 * half && lane < 32) lists[wave - half][lane] = list;
     __syncthreads();
-    if (wave < half) list = merge64(lane < 32 ? list : lds[wave][63 - lane], lane);
+    if (wave < half) list = merge64(lane < 32 ? list : lists[wave][63 - lane], lane);
   }
   return list;
 }
 
-struct Sums {
-  float M, S, W;  // maximum, sum of e = exp((x - M) / T), sum of e (x - M)
-};
-
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // below 2^-126: 0
 
-// The sums relative to a larger maximum M > -inf.  Where the factor is zero so is the weighted sum:
-// at distances near the type's lowest value S (a.M - M) overflows.  An empty side (maximum -inf)
-// holds zeros, or a NaN element's NaN, and keeps them.
-__device__ __forceinline__ Sums rebase(const Sums& a, float M, float c) {
-  if (a.M == -INFINITY) return {M, a.S, a.W};
-  const float d = a.M - M, f = exp2_fast(d * c);
-  return {M, a.S * f, f > 0.f ? (a.W + a.S * d) * f : 0.f};
+// Partial sums: the maximum M, the reference r = fl(M c), sum of e = 2^y and of e y, y = x c - r.
+// Where M c would overflow (rows of the type's lowest value), r is infinite and y = (x - M) c.
+struct Sums {
+  float M, r, S, W;
+};
+__device__ __forceinline__ float reference(float M, float c) {
+  const float r = M * c;
+  return fabsf(r) < 1e38f ? r : INFINITY;
+}
+__device__ __forceinline__ Sums empty_sums() { return {-INFINITY, 0.f, 0.f, 0.f}; }
+
+// The sums moved to the reference of a larger maximum M > -inf.  Where the factor is zero so is the
+// weighted sum: far below the maximum (the type's lowest value) S d overflows.  An empty side (maximum
+// -inf) holds zeros, or a NaN element's NaN, and keeps them.
+__device__ __forceinline__ Sums rebase(const Sums& a, float M, float r, float c) {
+  if (a.M == -INFINITY) return {M, r, a.S, a.W};
+  const float d = a.r < INFINITY && r < INFINITY ? a.r - r : (a.M - M) * c, f = exp2_fast(d);
+  return {M, r, a.S * f, f > 0.f ? (a.W + a.S * d) * f : 0.f};
 }
 
 // Two partial sums joined at their larger maximum.
 __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
-  const float M = fmaxf(a.M, b.M);
-  if (M == -INFINITY) return {M, a.S + b.S, a.W + b.W};
-  const Sums sa = rebase(a, M, c), sb = rebase(b, M, c);
-  return {M, sa.S + sb.S, sa.W + sb.W};
+  const float M = fmaxf(a.M, b.M), r = a.M >= b.M ? a.r : b.r;
+  if (M == -INFINITY) return {M, 0.f, a.S + b.S, a.W + b.W};
+  const Sums sa = a.M == M ? a : rebase(a, M, r, c), sb = b.M == M ? b : rebase(b, M, r, c);
+  return {M, r, sa.S + sb.S, sa.W + sb.W};
 }
 
 __device__ __forceinline__ Sums wave_join(Sums s, float c) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1)
-    s = join(s, Sums{__shfl_xor(s.M, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)}, c);
+    s = join(s, Sums{__shfl_xor(s.M, o, 64), __shfl_xor(s.r, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)}, c);
   return s;
 }
 
@@ -127,17 +156,16 @@ struct Args {
   uint64_t* keys;       // [m][splits][32]
 };
 
-__device__ __forceinline__ int64_t target_of(const LogprobFwd& p, int64_t row) { return p.targets ? p.targets[row] : 0; }
-
-// The row's results from its sums (all lanes of wave 0 call it; list: the top keys).
+// The row's results from its sums (all lanes of a wave call it; list: the top keys by lane).
 template <typename T>
 __device__ __forceinline__ void finish(const Args& a, int64_t row, const Sums& s, uint64_t list, int lane) {
   const LogprobFwd& p = a.p;
-  const bool dead = p.targets && p.targets[row] < 0;
-  const float log_s = s.M == -INFINITY && s.S == 0.f ? -INFINITY : logf(s.S);
-  const bool none = s.M == -INFINITY;
+  const bool dead = p.targets && p.targets[row] < 0, none = s.M == -INFINITY;
+  // off = M c - r: what the reference is off by, in the exponents' unit
+  const float ln2 = 0.69314718055994531f, off = none || s.r == INFINITY ? 0.f : fmaf(s.M, a.c, -s.r);
+  const float log_s = none && s.S == 0.f ? -INFINITY : fmaf(-off, ln2, logf(s.S));
   if (lane == 0) {
-    float H = none ? s.S : log_s - s.W / s.S * a.inv_t;
+    float H = none ? s.S : fmaf(off - s.W / s.S, ln2, log_s);
     if (H < 0.f) H = 0.f;
     p.stats[row * 3] = dead ? 0.f : s.M;
     p.stats[row * 3 + 1] = dead ? 0.f : log_s;
@@ -164,10 +192,6 @@ __device__ __forceinline__ void finish(const Args& a, int64_t row, const Sums& s
 template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   __shared__ Sums wave_sums[kWaves];
-  __shared__ uint64_t lists[kWaves][32];
-  __shared__ uint64_t bound_key;
-  __shared__ int n_owner;
-  __shared__ int owner[32];
   const int64_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool dead = a.p.targets && a.p.targets[row] < 0;
@@ -175,68 +199,111 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   const T* x = reinterpret_cast<const T*>(a.p.logits) + row * a.p.ld;
   const int64_t lo = split * a.len, hi = dead ? lo : min(a.p.V, lo + a.len);
 
-  Sums s{-INFINITY, 0.f, 0.f};
-  float best = -INFINITY;
-  int64_t best_at = 0;
-  for (int64_t i = lo + (int64_t)tid * kGroup; i < hi; i += kStep) {
+  Sums s = empty_sums();
+  float best = -INFINITY;  // the largest element of this lane, and the first index of its group
+  uint32_t best_at = 0;
+  auto add1 = [&](float y) {
+    const float e = exp2_fast(y);
+    s.S += e;
+    s.W = fmaf(e, fmaxf(y, -1e30f), s.W);  // -inf contributes 0, not 0 * -inf
+  };
+  auto add = [&](const float v[8]) {  // s.M is at least their maximum
+    if (s.r < INFINITY) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) add1(fmaf(v[j], a.c, -s.r));
+    } else {
+      for (int j = 0; j < 8; ++j) add1((v[j] - s.M) * a.c);
+    }
+  };
+  auto raise = [&](float M) {
+    if (M > s.M) s = rebase(s, M, reference(M, a.c), a.c);
+  };
+  auto group_max = [&](const float v[8], int64_t i) {
+    const float g = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    if constexpr (TOP)
+      if (g > best) {
+        best = g;
+        best_at = (uint32_t)i;
+      }
+    return g;
+  };
+  int64_t i = lo + (int64_t)tid * kGroup;
+  for (int64_t base = lo; base + kTrip <= hi; base += kTrip, i += kTrip) {  // whole trips: kUnroll groups in flight
+    float v[kUnroll][8], g = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) load8(x + i + u * kStep, v[u]);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) g = fmaxf(g, group_max(v[u], i + u * kStep));
+    raise(g);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) add(v[u]);
+  }
+  for (; i < hi; i += kStep) {
     float v[8];
     load_upto8(x + i, (int)min((int64_t)8, hi - i), -INFINITY, v);
-    float g = v[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) g = fmaxf(g, v[j]);
-    if (g > best) { best = g; best_at = i; }
-    const float M = fmaxf(s.M, g);
-    const float base = M == -INFINITY ? 0.f : M;
-    if (M > s.M) s = rebase(s, M, a.c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float dj = v[j] - base, e = exp2_fast(dj * a.c);
-      s.S += e;
-      s.W = fmaf(e, fmaxf(dj, -3.4028234663852886e38f), s.W);
-    }
-  }
-  uint64_t mine = 0ull;
-  if constexpr (TOP) {
-    if (best > -INFINITY) {
-      float v[8];
-      load_upto8(x + best_at, (int)min((int64_t)8, hi - best_at), -INFINITY, v);
-      int at = 0;
-#pragma unroll
-      for (int j = 7; j >= 0; --j)
-        if (v[j] == best) at = j;
-      mine = top_key(best, (uint32_t)(best_at + at));
-    }
+    raise(group_max(v, i));
+    add(v);
   }
   s = wave_join(s, a.c);
   if (lane == 0) wave_sums[wave] = s;
-  if (tid == 0) n_owner = 0;
-  __syncthreads();
-  if (wave == 0) {
-    s = lane < kWaves ? wave_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
-    s = wave_join(s, a.c);
+  __shared__ uint64_t maxima[TOP ? 64 : 1], lists[TOP ? kWaves / 2 : 1][32], joined[TOP ? 32 : 1], found[TOP ? kWaves : 1][128];
+  __shared__ int counts[kWaves];
+  [[maybe_unused]] uint64_t mine = 0ull;
+  if constexpr (TOP) {
+    static_assert(kThreads == 8 * 64, "64 maxima of eight lanes");
+    mine = top_key(best, best_at);
+    uint64_t g = max(mine, lane_xor<1>(mine, lane));
+    g = max(g, lane_xor<2>(g, lane));
+    g = max(g, lane_xor<4>(g, lane));
+    if (lane % 8 == 0) maxima[tid / 8] = g;
   }
+  __syncthreads();
+  if (wave == 0) s = wave_join(lane < kWaves ? wave_sums[lane] : empty_sums(), a.c);
   uint64_t list = 0ull;
   if constexpr (TOP) {
-    list = join_waves(sort64(mine, lane), lists, lane, wave);
-    if (wave == 0 && lane == a.p.top_k - 1) bound_key = list;
-    __syncthreads();
-    const uint64_t bound = bound_key;
-    // the lanes whose largest element is among the k largest of them
-    if (mine != 0ull && mine >= bound) owner[atomicAdd(&n_owner, 1)] = tid;
-    __syncthreads();
-    const int owners = n_owner;
-    const int64_t trips = (hi - lo + kStep - 1) / kStep;
-    list = 0ull;
-    for (int o = wave; o < owners; o += kWaves) {
-      const int64_t first = lo + (int64_t)owner[o] * kGroup;
-      for (int64_t t = 0; t < trips; t += 64 / kGroup) {  // 64 elements: eight groups of this owner
-        const int64_t i = first + (t + lane / kGroup) * kStep + lane % kGroup;
-        uint64_t k = 0ull;
-        if (t + lane / kGroup < trips && i < hi) k = top_key(load1(x + i), (uint32_t)i);
-        list = take64(list, k >= bound ? k : 0ull, lane);
+    // The bound: the k-th largest of the 64 largest keys of eight lanes each.  As an element's key, the
+    // last index of the bounding group: no element of that group is below it.
+    const uint64_t last = __shfl(sort64(maxima[lane], lane), a.p.top_k - 1, 64);
+    const uint64_t bound = last == 0ull ? 1ull : last - 7;
+    // Every wave looks through the elements of its own lanes whose largest is not below.
+    const int64_t groups = (hi - lo + kStep - 1) / kStep;  // of a lane
+    int n_found = 0;
+    bool overflow = false;
+    for (uint64_t owners = __ballot(mine != 0ull && mine >= last); owners != 0ull; owners &= owners - 1) {
+      const int64_t first = lo + (int64_t)(tid - lane + __builtin_ctzll(owners)) * kGroup + lane % kGroup;
+      for (int64_t t0 = 0; t0 < groups; t0 += 64 / kGroup) {  // eight groups at a time
+        const int64_t t = t0 + lane / kGroup, at = first + t * kStep;
+        const uint64_t k = t < groups && at < hi ? top_key(load1(x + at), (uint32_t)at) : 0ull;
+        const uint64_t hit = __ballot(k >= bound);
+        if (k >= bound) found[wave][n_found + __popcll(hit & ((1ull << lane) - 1))] = k;
+        n_found += __popcll(hit);
+        if (n_found >= 64) {  // many near the bound: keep the largest 32
+          list = take64(list, found[wave][lane], lane);
+          overflow = true;
+          n_found -= 64;
+          if (lane < n_found) found[wave][lane] = found[wave][64 + lane];
+        }
       }
     }
-    list = join_waves(list, lists, lane, wave);
+    if (lane == 0) counts[wave] = overflow ? -1 : n_found;
+    if (tid < 32) joined[tid] = 0ull;
+    __syncthreads();
+    bool any = false;
+    for (int w = 0; w < kWaves; ++w) any |= counts[w] < 0;
+    if (any) {
+      if (n_found > 0) list = take64(list, lane < n_found ? found[wave][lane] : 0ull, lane);
+      list = join_lists(list, lists, tid);
+    } else {  // the usual case, about k candidates: a key's place is the number of larger ones
+      if (lane < n_found) {
+        const uint64_t key = found[wave][lane];
+        int place = 0;
+        for (int w = 0; w < kWaves; ++w)
+          for (int i = 0; i < counts[w]; ++i) place += found[w][i] > key ? 1 : 0;
+        if (place < 32) joined[place] = key;
+      }
+      __syncthreads();
+      list = lane < 32 ? joined[lane] : 0ull;
+    }
   }
   if (wave != 0) return;
   if (a.splits == 1) {
@@ -247,23 +314,27 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   }
 }
 
-// Joins the splits of a row: one wave per row.
+// Joins the splits of a row: a workgroup per row, its waves every kWaves-th split.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(64) void logprob_join_kernel(Args a) {
+__global__ __launch_bounds__(kThreads) void logprob_join_kernel(Args a) {
   const int64_t row = blockIdx.x;
-  const int lane = threadIdx.x;
-  Sums s{-INFINITY, 0.f, 0.f};
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool dead = a.p.targets && a.p.targets[row] < 0;
   uint64_t list = 0ull;
-  if (!(a.p.targets && a.p.targets[row] < 0)) {
-    for (int64_t i = lane; i < a.splits; i += 64) s = join(s, a.sums[row * a.splits + i], a.c);
-    s = wave_join(s, a.c);
-    if constexpr (TOP)
-      for (int64_t i = 0; i < a.splits * 32; i += 64) {
-        const uint64_t k = i + lane < a.splits * 32 ? a.keys[row * a.splits * 32 + i + lane] : 0ull;
-        list = take64(list, k, lane);
+  if constexpr (TOP) {
+    __shared__ uint64_t lists[kWaves / 2][32];
+    if (!dead)
+      for (int64_t i = wave; i < a.splits; i += kWaves) {
+        const uint64_t* src = a.keys + (row * a.splits + i) * 32;
+        list = merge64(lane < 32 ? list : src[63 - lane], lane);
       }
+    list = join_lists(list, lists, tid);
   }
-  finish<T>(a, row, s, list, lane);
+  if (wave != 0) return;
+  Sums s = empty_sums();
+  if (!dead)
+    for (int64_t i = lane; i < a.splits; i += 64) s = join(s, a.sums[row * a.splits + i], a.c);
+  finish<T>(a, row, wave_join(s, a.c), list, lane);
 }
 
 // Workgroups per row: enough to give every CU four, none with less than one trip.
@@ -337,7 +408,7 @@ void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStrea
 #define RESQ_LP(T, K)                                                                          \
   do {                                                                                         \
     launch_timed(logprob_kernel<T, K>, grid, dim3(kThreads), 0u, s, a);                        \
-    if (a.splits > 1) launch_timed(logprob_join_kernel<T, K>, joins, dim3(64), 0u, s, a);      \
+    if (a.splits > 1) launch_timed(logprob_join_kernel<T, K>, joins, dim3(kThreads), 0u, s, a);\
   } while (0)
   if (f32) { if (p.top_k > 0) RESQ_LP(float, true); else RESQ_LP(float, false); }
   else { if (p.top_k > 0) RESQ_LP(uint16_t, true); else RESQ_LP(uint16_t, false); }
