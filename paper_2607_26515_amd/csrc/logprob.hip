@@ -29,11 +29,11 @@
 namespace resq {
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kGroup = 8;                            // elements per load
-constexpr int64_t kStep = (int64_t)kThreads * kGroup;  // elements that a workgroup's lanes load at once
-constexpr int kUnroll = 4;
-constexpr int64_t kTrip = kStep * kUnroll;
+constexpr int kGroup = 8;   // elements per load
+constexpr int kUnroll = 4;  // loads in flight per lane
+// Waves per workgroup: 8, or 2 for short rows (8192 x 2000, top 5: 90 us with 8).
+constexpr int kShortRow = 8192;
+int waves_for(int64_t V) { return V <= kShortRow ? 2 : 8; }
 
 // Descending order of values as ascending-free unsigned keys: larger value, then lower index.
 // -inf and NaN are no alternatives: key 0.
@@ -100,9 +100,10 @@ __device__ __forceinline__ uint64_t take64(uint64_t list, uint64_t more, int lan
 
 // Joins the waves' descending lists (lanes 0..31 of each) in wave 0, halving the waves.  Every wave
 // must call it.
+template <int W>
 __device__ __forceinline__ uint64_t join_lists(uint64_t list, uint64_t (*lists)[32], int tid) {
   const int lane = tid & 63, wave = tid >> 6;
-  for (int half = kWaves / 2; half > 0; half >>= 1) {
+  for (int half = W / 2; half > 0; half >>= 1) {
     __syncthreads();
     if (wave >= half && wave < 2 * half && lane < 32) lists[wave - half][lane] = list;
     __syncthreads();
@@ -113,45 +114,72 @@ __device__ __forceinline__ uint64_t join_lists(uint64_t list, uint64_t (*lists)[
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // below 2^-126: 0
 
-// Partial sums: the maximum M, the reference r = fl(M c), sum of e = 2^y and of e y, y = x c - r.
-// Where M c would overflow (rows of the type's lowest value), r is infinite and y = (x - M) c.
-struct Sums {
-  float M, r, S, W;
-};
+// fmaxf quiets its operands first, an instruction each; these take them as they are (the maximum of a
+// NaN and a number is the number).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+  float r;
+  asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// The reference of a maximum M, r = fl(M c); infinite where M c would overflow (rows of the type's
+// lowest value): there y = (x - M) c.
 __device__ __forceinline__ float reference(float M, float c) {
   const float r = M * c;
   return fabsf(r) < 1e38f ? r : INFINITY;
 }
-__device__ __forceinline__ Sums empty_sums() { return {-INFINITY, 0.f, 0.f, 0.f}; }
 
-// The sums moved to the reference of a larger maximum M > -inf.  Where the factor is zero so is the
-// weighted sum: far below the maximum (the type's lowest value) S d overflows.  An empty side (maximum
-// -inf) holds zeros, or a NaN element's NaN, and keeps them.
-__device__ __forceinline__ Sums rebase(const Sums& a, float M, float r, float c) {
-  if (a.M == -INFINITY) return {M, r, a.S, a.W};
-  const float d = a.r < INFINITY && r < INFINITY ? a.r - r : (a.M - M) * c, f = exp2_fast(d);
-  return {M, r, a.S * f, f > 0.f ? (a.W + a.S * d) * f : 0.f};
+// Partial sums: the maximum M, the sums of e = 2^y and of e y, y = x c - reference(M, c).
+struct Sums {
+  float M, S, W;
+};
+__device__ __forceinline__ Sums empty_sums() { return {-INFINITY, 0.f, 0.f}; }
+
+// The sums moved to a maximum M >= a.M.  Where the factor is zero so is the weighted sum: far below the
+// maximum S d overflows.  An empty side (maximum -inf) holds zeros, or a NaN element's NaN, and keeps
+// them.
+__device__ __forceinline__ Sums rebase(const Sums& a, float M, float c) {
+  if (a.M == -INFINITY || a.M == M) return {M, a.S, a.W};
+  const float ra = reference(a.M, c), r = reference(M, c);
+  const float d = ra < INFINITY && r < INFINITY ? ra - r : (a.M - M) * c, f = exp2_fast(d);
+  return {M, a.S * f, f > 0.f ? (a.W + a.S * d) * f : 0.f};
 }
 
-// Two partial sums joined at their larger maximum.
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
-  const float M = fmaxf(a.M, b.M), r = a.M >= b.M ? a.r : b.r;
-  if (M == -INFINITY) return {M, 0.f, a.S + b.S, a.W + b.W};
-  const Sums sa = a.M == M ? a : rebase(a, M, r, c), sb = b.M == M ? b : rebase(b, M, r, c);
-  return {M, r, sa.S + sb.S, sa.W + sb.W};
+__device__ __forceinline__ float xor16_32(float v, int lane, bool max) {
+  const float o = __uint_as_float(lane_xor<16>(__float_as_uint(v), lane));
+  v = max ? max2(v, o) : v + o;
+  const float p = __uint_as_float(lane_xor<32>(__float_as_uint(v), lane));
+  return max ? max2(v, p) : v + p;
 }
-
-__device__ __forceinline__ Sums wave_join(Sums s, float c) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-    s = join(s, Sums{__shfl_xor(s.M, o, 64), __shfl_xor(s.r, o, 64), __shfl_xor(s.S, o, 64), __shfl_xor(s.W, o, 64)}, c);
-  return s;
+// Maximum, or sum in a fixed order, over the wave.
+__device__ __forceinline__ float wave_max(float v, int lane) {
+  v = max2(v, dpp<kDppXor1>(v));
+  v = max2(v, dpp<kDppXor2>(v));
+  v = max2(v, dpp<kDppHalfMirror>(v));
+  v = max2(v, dpp<kDppMirror>(v));
+  return xor16_32(v, lane, true);
+}
+__device__ __forceinline__ float wave_sum(float v, int lane) {
+  v += dpp<kDppXor1>(v);
+  v += dpp<kDppXor2>(v);
+  v += dpp<kDppHalfMirror>(v);
+  v += dpp<kDppMirror>(v);
+  return xor16_32(v, lane, false);
+}
+__device__ __forceinline__ Sums wave_join(const Sums& a, float c, int lane) {
+  const Sums s = rebase(a, wave_max(a.M, lane), c);
+  return {s.M, wave_sum(s.S, lane), wave_sum(s.W, lane)};
 }
 
 struct Args {
   LogprobFwd p;
   float c, inv_t;       // log2(e) / T, 1 / T
-  int64_t splits, len;  // workgroups per row, elements each (a multiple of kStep)
+  int64_t splits, len;  // workgroups per row, elements each
   Sums* sums;           // [m][splits]
   uint64_t* keys;       // [m][splits][32]
 };
@@ -162,7 +190,8 @@ __device__ __forceinline__ void finish(const Args& a, int64_t row, const Sums& s
   const LogprobFwd& p = a.p;
   const bool dead = p.targets && p.targets[row] < 0, none = s.M == -INFINITY;
   // off = M c - r: what the reference is off by, in the exponents' unit
-  const float ln2 = 0.69314718055994531f, off = none || s.r == INFINITY ? 0.f : fmaf(s.M, a.c, -s.r);
+  const float ln2 = 0.69314718055994531f, r = reference(s.M, a.c);
+  const float off = none || r == INFINITY ? 0.f : fmaf(s.M, a.c, -r);
   const float log_s = none && s.S == 0.f ? -INFINITY : fmaf(-off, ln2, logf(s.S));
   if (lane == 0) {
     float H = none ? s.S : fmaf(off - s.W / s.S, ln2, log_s);
@@ -188,38 +217,47 @@ __device__ __forceinline__ void finish(const Args& a, int64_t row, const Sums& s
   }
 }
 
-// One workgroup per row and split.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
-  __shared__ Sums wave_sums[kWaves];
+// One workgroup of W waves per row and split.
+template <typename T, bool TOP, int W>
+__global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
+  constexpr int kStep = 64 * W * kGroup, kTrip = kStep * kUnroll;
+  __shared__ Sums wave_sums[W];
+  __shared__ uint64_t maxima[TOP ? 64 : 1], lists[TOP ? W / 2 : 1][32], joined[TOP ? 32 : 1], found[TOP ? W : 1][128];
+  __shared__ int counts[W];
   const int64_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool dead = a.p.targets && a.p.targets[row] < 0;
   if (dead && a.splits > 1) return;
   const T* x = reinterpret_cast<const T*>(a.p.logits) + row * a.p.ld;
-  const int64_t lo = split * a.len, hi = dead ? lo : min(a.p.V, lo + a.len);
+  // Groups start at 16-byte boundaries: the elements before the first are one more group, of lane 0.
+  const int head = dead ? 0 : (int)min(a.p.V, (int64_t)((-(uintptr_t)x & 15u) / sizeof(T)));
+  const int64_t lo = dead ? 0 : head + split * a.len, hi = dead ? 0 : min(a.p.V, lo + a.len);
 
   Sums s = empty_sums();
+  float r = 0.f;           // reference(s.M)
   float best = -INFINITY;  // the largest element of this lane, and the first index of its group
   uint32_t best_at = 0;
   auto add1 = [&](float y) {
     const float e = exp2_fast(y);
     s.S += e;
-    s.W = fmaf(e, fmaxf(y, -1e30f), s.W);  // -inf contributes 0, not 0 * -inf
+    s.W = fmaf(e, max2(y, -1e30f), s.W);  // -inf contributes 0, not 0 * -inf
   };
   auto add = [&](const float v[8]) {  // s.M is at least their maximum
-    if (s.r < INFINITY) {
+    if (r < INFINITY) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) add1(fmaf(v[j], a.c, -s.r));
+      for (int j = 0; j < 8; ++j) add1(fmaf(v[j], a.c, -r));
     } else {
       for (int j = 0; j < 8; ++j) add1((v[j] - s.M) * a.c);
     }
   };
   auto raise = [&](float M) {
-    if (M > s.M) s = rebase(s, M, reference(M, a.c), a.c);
+    if (M > s.M) {
+      s = rebase(s, M, a.c);
+      r = reference(M, a.c);
+    }
   };
   auto group_max = [&](const float v[8], int64_t i) {
-    const float g = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    const float g = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max2(v[6], v[7]));
     if constexpr (TOP)
       if (g > best) {
         best = g;
@@ -227,13 +265,19 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
       }
     return g;
   };
+  if (split == 0 && tid == 0 && head > 0) {
+    float v[8];
+    load_upto8(x, head, -INFINITY, v);
+    raise(group_max(v, 0));
+    add(v);
+  }
   int64_t i = lo + (int64_t)tid * kGroup;
   for (int64_t base = lo; base + kTrip <= hi; base += kTrip, i += kTrip) {  // whole trips: kUnroll groups in flight
     float v[kUnroll][8], g = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) load8(x + i + u * kStep, v[u]);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) g = fmaxf(g, group_max(v[u], i + u * kStep));
+    for (int u = 0; u < kUnroll; ++u) g = max2(g, group_max(v[u], i + u * kStep));
     raise(g);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) add(v[u]);
@@ -244,60 +288,62 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
     raise(group_max(v, i));
     add(v);
   }
-  s = wave_join(s, a.c);
+  s = wave_join(s, a.c, lane);
   if (lane == 0) wave_sums[wave] = s;
-  __shared__ uint64_t maxima[TOP ? 64 : 1], lists[TOP ? kWaves / 2 : 1][32], joined[TOP ? 32 : 1], found[TOP ? kWaves : 1][128];
-  __shared__ int counts[kWaves];
   [[maybe_unused]] uint64_t mine = 0ull;
-  if constexpr (TOP) {
-    static_assert(kThreads == 8 * 64, "64 maxima of eight lanes");
+  if constexpr (TOP) {  // the largest keys of W lanes each
     mine = top_key(best, best_at);
-    uint64_t g = max(mine, lane_xor<1>(mine, lane));
-    g = max(g, lane_xor<2>(g, lane));
-    g = max(g, lane_xor<4>(g, lane));
-    if (lane % 8 == 0) maxima[tid / 8] = g;
+    uint64_t g = mine;
+    if constexpr (W >= 2) g = max(g, lane_xor<1>(g, lane));
+    if constexpr (W >= 4) g = max(g, lane_xor<2>(g, lane));
+    if constexpr (W >= 8) g = max(g, lane_xor<4>(g, lane));
+    if (lane % W == 0) maxima[tid / W] = g;
   }
   __syncthreads();
-  if (wave == 0) s = wave_join(lane < kWaves ? wave_sums[lane] : empty_sums(), a.c);
+  if (wave == 0) s = wave_join(lane < W ? wave_sums[lane] : empty_sums(), a.c, lane);
   uint64_t list = 0ull;
   if constexpr (TOP) {
-    // The bound: the k-th largest of the 64 largest keys of eight lanes each.  As an element's key, the
-    // last index of the bounding group: no element of that group is below it.
+    // The bound: the k-th largest of the 64 maxima.  As an element's key, the last index of the
+    // bounding group: no element of that group is below it.
     const uint64_t last = __shfl(sort64(maxima[lane], lane), a.p.top_k - 1, 64);
     const uint64_t bound = last == 0ull ? 1ull : last - 7;
     // Every wave looks through the elements of its own lanes whose largest is not below.
-    const int64_t groups = (hi - lo + kStep - 1) / kStep;  // of a lane
     int n_found = 0;
     bool overflow = false;
-    for (uint64_t owners = __ballot(mine != 0ull && mine >= last); owners != 0ull; owners &= owners - 1) {
-      const int64_t first = lo + (int64_t)(tid - lane + __builtin_ctzll(owners)) * kGroup + lane % kGroup;
-      for (int64_t t0 = 0; t0 < groups; t0 += 64 / kGroup) {  // eight groups at a time
-        const int64_t t = t0 + lane / kGroup, at = first + t * kStep;
-        const uint64_t k = t < groups && at < hi ? top_key(load1(x + at), (uint32_t)at) : 0ull;
-        const uint64_t hit = __ballot(k >= bound);
-        if (k >= bound) found[wave][n_found + __popcll(hit & ((1ull << lane) - 1))] = k;
-        n_found += __popcll(hit);
-        if (n_found >= 64) {  // many near the bound: keep the largest 32
-          list = take64(list, found[wave][lane], lane);
-          overflow = true;
-          n_found -= 64;
-          if (lane < n_found) found[wave][lane] = found[wave][64 + lane];
-        }
+    auto consider = [&](uint64_t k) {
+      const uint64_t hit = __ballot(k >= bound);
+      if (k >= bound) found[wave][n_found + __popcll(hit & ((1ull << lane) - 1))] = k;
+      n_found += __popcll(hit);
+      if (n_found >= 64) {  // many near the bound: keep the largest 32
+        list = take64(list, found[wave][lane], lane);
+        overflow = true;
+        n_found -= 64;
+        if (lane < n_found) found[wave][lane] = found[wave][64 + lane];
+      }
+    };
+    uint64_t owners = __ballot(mine != 0ull && mine >= last);
+    if (split == 0 && wave == 0 && head > 0 && (owners & 1))
+      consider(lane < head ? top_key(load1(x + lane), (uint32_t)lane) : 0ull);
+    for (; owners != 0ull; owners &= owners - 1) {
+      const int64_t first = lo + (int64_t)(tid - lane + __builtin_ctzll(owners)) * kGroup;
+      for (int64_t t0 = first; t0 < hi; t0 += 64 / kGroup * kStep) {  // eight groups at a time
+        const int64_t at = t0 + lane / kGroup * kStep + lane % kGroup;
+        consider(at < hi ? top_key(load1(x + at), (uint32_t)at) : 0ull);
       }
     }
     if (lane == 0) counts[wave] = overflow ? -1 : n_found;
     if (tid < 32) joined[tid] = 0ull;
     __syncthreads();
     bool any = false;
-    for (int w = 0; w < kWaves; ++w) any |= counts[w] < 0;
+    for (int w = 0; w < W; ++w) any |= counts[w] < 0;
     if (any) {
       if (n_found > 0) list = take64(list, lane < n_found ? found[wave][lane] : 0ull, lane);
-      list = join_lists(list, lists, tid);
+      list = join_lists<W>(list, lists, tid);
     } else {  // the usual case, about k candidates: a key's place is the number of larger ones
       if (lane < n_found) {
         const uint64_t key = found[wave][lane];
         int place = 0;
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < W; ++w)
           for (int i = 0; i < counts[w]; ++i) place += found[w][i] > key ? 1 : 0;
         if (place < 32) joined[place] = key;
       }
@@ -314,39 +360,44 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(Args a) {
   }
 }
 
-// Joins the splits of a row: a workgroup per row, its waves every kWaves-th split.
+// Joins the splits of a row: a workgroup per row, its waves every kJoinWaves-th split.
+constexpr int kJoinWaves = 8;
 template <typename T, bool TOP>
-__global__ __launch_bounds__(kThreads) void logprob_join_kernel(Args a) {
+__global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(Args a) {
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool dead = a.p.targets && a.p.targets[row] < 0;
   uint64_t list = 0ull;
   if constexpr (TOP) {
-    __shared__ uint64_t lists[kWaves / 2][32];
+    __shared__ uint64_t lists[kJoinWaves / 2][32];
     if (!dead)
-      for (int64_t i = wave; i < a.splits; i += kWaves) {
+      for (int64_t i = wave; i < a.splits; i += kJoinWaves) {
         const uint64_t* src = a.keys + (row * a.splits + i) * 32;
         list = merge64(lane < 32 ? list : src[63 - lane], lane);
       }
-    list = join_lists(list, lists, tid);
+    list = join_lists<kJoinWaves>(list, lists, tid);
   }
   if (wave != 0) return;
   Sums s = empty_sums();
   if (!dead)
-    for (int64_t i = lane; i < a.splits; i += 64) s = join(s, a.sums[row * a.splits + i], a.c);
-  finish<T>(a, row, wave_join(s, a.c), list, lane);
+    for (int64_t i = 0; i < a.splits; i += 64) {
+      const Sums t = wave_join(i + lane < a.splits ? a.sums[row * a.splits + i + lane] : empty_sums(), a.c, lane);
+      const float M = max2(s.M, t.M);
+      const Sums sa = rebase(s, M, a.c), sb = rebase(t, M, a.c);
+      s = {M, sa.S + sb.S, sa.W + sb.W};
+    }
+  finish<T>(a, row, s, list, lane);
 }
 
-// Workgroups per row: enough to give every CU four, none with less than one trip.
+// Workgroups per row: enough to give every CU four, none with less than a load per lane.
 int64_t splits_of(int64_t m, int64_t V) {
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(m, 1));
-  const int64_t trips = (V + kStep - 1) / kStep;
-  const int64_t per = (trips + want - 1) / want;
+  const int64_t step = 64 * kGroup * waves_for(V), want = std::max<int64_t>(1, 1024 / std::max<int64_t>(m, 1));
+  const int64_t trips = (V + step - 1) / step, per = (trips + want - 1) / want;
   return (trips + per - 1) / per;
 }
 int64_t split_len(int64_t V, int64_t splits) {
-  const int64_t trips = (V + kStep - 1) / kStep;
-  return (trips + splits - 1) / splits * kStep;
+  const int64_t step = 64 * kGroup * waves_for(V), trips = (V + step - 1) / step;
+  return (trips + splits - 1) / splits * step;
 }
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
@@ -407,8 +458,9 @@ void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStrea
   const dim3 grid((unsigned)(p.m * a.splits)), joins((unsigned)p.m);
 #define RESQ_LP(T, K)                                                                          \
   do {                                                                                         \
-    launch_timed(logprob_kernel<T, K>, grid, dim3(kThreads), 0u, s, a);                        \
-    if (a.splits > 1) launch_timed(logprob_join_kernel<T, K>, joins, dim3(kThreads), 0u, s, a);\
+    if (waves_for(p.V) == 2) launch_timed(logprob_kernel<T, K, 2>, grid, dim3(128), 0u, s, a); \
+    else launch_timed(logprob_kernel<T, K, 8>, grid, dim3(512), 0u, s, a);                     \
+    if (a.splits > 1) launch_timed(logprob_join_kernel<T, K>, joins, dim3(512), 0u, s, a);     \
   } while (0)
   if (f32) { if (p.top_k > 0) RESQ_LP(float, true); else RESQ_LP(float, false); }
   else { if (p.top_k > 0) RESQ_LP(uint16_t, true); else RESQ_LP(uint16_t, false); }
