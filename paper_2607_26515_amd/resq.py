@@ -570,111 +570,123 @@ def linear_fwd_swiglu(g, u, wprep, n, fmt, sparsity, y=None, ws=None, stream=Non
 # ------------------------------------------------------------------------------------------
 # operators around the linears
 # ------------------------------------------------------------------------------------------
+# (These helpers run on every call of operators whose kernels take a few microseconds: one pass over
+# each tensor's properties, torch looked up once.)
+_torch = None
+_CODES = {}   # element type -> library code
+_TYPES = {}   # library code -> element type of outputs
+_handle = [None]  # device index -> handle of its current stream
+
+
+def _th():
+    global _torch
+    if _torch is None:
+        import torch
+        _CODES.update({torch.float32: IN_F32, torch.bfloat16: IN_BF16, torch.int16: IN_BF16, torch.uint16: IN_BF16})
+        _TYPES.update({IN_F32: torch.float32, IN_BF16: torch.bfloat16})
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # the handle without a Stream object
+        _handle[0] = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _torch = torch
+    return _torch
+
+
 def _dtype(t, what) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return IN_F32
-    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
-        return IN_BF16
-    raise TypeError(f"{what} must be float32 or bfloat16 (or its 16-bit patterns), not {t.dtype}")
-
-
-def _like(dtype_code):
-    import torch
-    return torch.float32 if dtype_code == IN_F32 else torch.bfloat16
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16 (or its 16-bit patterns), not {t.dtype}")
+    return code
 
 
 def _out_code(out) -> int:
-    if out not in ("f32", "bf16"):
-        raise ValueError(f"out must be 'f32' or 'bf16', not {out!r}")
-    return IN_F32 if out == "f32" else IN_BF16
+    if out == "bf16":
+        return IN_BF16
+    if out == "f32":
+        return IN_F32
+    raise ValueError(f"out must be 'f32' or 'bf16', not {out!r}")
 
 
-def _rows(t, what, m, d, dev) -> int:
-    """The row stride of an m x d device matrix with unit column stride."""
-    if t.device != dev:
-        raise ValueError(f"{what} is on {t.device}, not on {dev}")
-    if t.dim() != 2 or t.shape[0] != m or t.shape[1] != d:
+def _matrix(t, what):
+    """(m, d, device index) of a matrix."""
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be a matrix")
+    m, d = t.shape
+    return m, d, t.get_device()
+
+
+def _rows(t, what, m, d, index) -> int:
+    """The row stride of an m x d matrix on that device, with unit column stride."""
+    if t.shape != (m, d):
         raise ValueError(f"{what} must be {m} x {d}, not {tuple(t.shape)}")
-    if d > 1 and t.stride(1) != 1:
+    if t.get_device() != index:
+        raise ValueError(f"{what} is not on the device of the first argument")
+    ld, step = t.stride()
+    if step != 1 and d > 1:
         raise ValueError(f"{what} must have unit column stride")
     if m <= 1:
         return d
-    if t.stride(0) < d:
-        raise ValueError(f"{what} has overlapping rows (stride {t.stride(0)} < {d})")
-    return t.stride(0)
+    if ld < d:
+        raise ValueError(f"{what} has overlapping rows (stride {ld} < {d})")
+    return ld
 
 
-def _vector(t, what, n, dtypes, dev):
+def _vector(t, what, n, code, index) -> int:
+    """The address of n contiguous values of a type (a library code, or an element type)."""
     if t is None:
         return 0
-    if t.device != dev:
-        raise ValueError(f"{what} is on {t.device}, not on {dev}")
-    if t.dtype not in dtypes:
+    if t.dtype is not code and (_CODES.get(t.dtype, -1) != code):
         raise TypeError(f"{what} has type {t.dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{what} is not on the device of the first argument")
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must hold {n} contiguous values")
     return t.data_ptr()
 
 
-class _On:
-    """The device and stream a call runs on: `stream`, or the current one of the tensor's device.
-    Inside, torch allocates for that stream."""
-
-    def __init__(self, t, stream):
-        import torch
-        if t.device.type != "cuda":
-            raise ValueError(f"tensors must be on a GPU, not on {t.device}")
-        self.ctx = None
-        if stream is not None:
-            if stream.device != t.device:
-                raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
-            self.ctx = torch.cuda.stream(stream)
-        elif t.device.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(t.device)
-
-    def __enter__(self):
-        import torch
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _enter(index, stream):
+    """(context or None, stream handle): the device and stream a call runs on, `stream` or the current
+    one of the tensors' device.  Inside the context torch allocates for that stream."""
+    torch = _torch
+    if index < 0:
+        raise ValueError("tensors must be on a GPU")
+    if stream is None:
+        if torch.cuda.current_device() == index:
+            return None, _handle[0](index)
+        ctx = torch.cuda.device(index)
+    else:
+        if stream.device.index != index:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on cuda:{index}")
+        ctx = torch.cuda.stream(stream)
+    ctx.__enter__()
+    return ctx, _handle[0](index)
 
 
-def _workspace(op, m, d, n, dev):
-    """(tensor, pointer, bytes): allocated on the current stream."""
-    import torch
-    nb = load().resq_workspace_size(op, 0, 0, m, d, n)
-    t = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
-    return t, _p(t), nb
-
-
-def _ws_arg(ws, op, m, d, n, dev):
+def _ws_arg(lib, ws, op, m, d, n, dev):
+    """(tensor, address, bytes) of a workspace: the caller's, or one allocated on the current stream."""
     if ws is None:
-        return _workspace(op, m, d, n, dev)
+        nb = lib.resq_workspace_size(op, 0, 0, m, d, n)
+        if nb == 0:
+            return None, 0, 0
+        ws = _torch.empty(nb, dtype=_torch.uint8, device=dev), nb
     buf, nb = ws
     if buf.device != dev:
         raise ValueError(f"the workspace is on {buf.device}, not on {dev}")
-    return buf, _p(buf), nb
+    return buf, buf.data_ptr(), nb
 
 
-def _gate_args(gate, m, d, dev):
-    """(pointer, dtype, mode): d values (or 1 x d) per channel, m x 1 per token."""
+def _gate_args(gate, m, d, index):
+    """(address, dtype, mode): d values (or 1 x d) per channel, m x 1 per token."""
     if gate is None:
         return 0, IN_BF16, GATE_NONE
-    if gate.device != dev:
-        raise ValueError(f"gate is on {gate.device}, not on {dev}")
+    if gate.get_device() != index:
+        raise ValueError("gate is not on the device of the first argument")
     if not gate.is_contiguous():
         raise ValueError("gate must be contiguous")
-    shape = tuple(gate.shape)
-    if shape == (d,) or (shape == (1, d) and not (m == 1 and d == 1)):
-        return gate.data_ptr(), _dtype(gate, "gate"), GATE_CHANNEL
+    shape = gate.shape
     if shape == (m, 1):
         return gate.data_ptr(), _dtype(gate, "gate"), GATE_TOKEN
-    raise ValueError(f"gate must have shape ({d},) or ({m}, 1), not {shape}")
+    if shape == (d,) or shape == (1, d):
+        return gate.data_ptr(), _dtype(gate, "gate"), GATE_CHANNEL
+    raise ValueError(f"gate must have shape ({d},) or ({m}, 1), not {tuple(shape)}")
 
 
 def block_norm(h, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None, eps=1e-6, save=True, h_out=None,
@@ -685,35 +697,37 @@ def block_norm(h, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None,
     norm there), gate d values (per channel) or m x 1 (per token).  h_out may be h (in place).
     Returns (h_out, x, rstd): x bfloat16 (None without gamma_pre), rstd the 2 x m row factors that
     block_norm_bwd takes (None with save=False).  Without y: the norm of h alone, h_out is h."""
-    import torch
-    if h.dim() != 2:
-        raise ValueError("h must be a matrix")
-    m, d = h.shape
-    dev = h.device
-    bits = (torch.bfloat16, torch.int16, torch.uint16)
-    hd, ldh = _dtype(h, "h"), _rows(h, "h", m, d, dev)
-    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, dev))
-    g, gd, gm = _gate_args(gate, m, d, dev)
-    gpost, gpre = _vector(gamma_post, "gamma_post", d, bits, dev), _vector(gamma_pre, "gamma_pre", d, bits, dev)
-    with _On(h, stream) as s:
+    torch, lib = _th(), load()
+    m, d, index = _matrix(h, "h")
+    hd, ldh = _dtype(h, "h"), _rows(h, "h", m, d, index)
+    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, index))
+    g, gd, gm = _gate_args(gate, m, d, index)
+    gpost, gpre = _vector(gamma_post, "gamma_post", d, IN_BF16, index), _vector(gamma_pre, "gamma_pre", d, IN_BF16, index)
+    ctx, s = _enter(index, stream)
+    try:
         if y is None:
-            h_out = h
+            h_out, ldho = h, ldh
         elif h_out is None:
-            h_out = torch.empty((m, d), dtype=h.dtype, device=dev)
-        elif h_out.dtype != h.dtype:
-            raise TypeError(f"h_out has type {h_out.dtype}, h {h.dtype}")
-        ldho = _rows(h_out, "h_out", m, d, dev)
+            h_out, ldho = torch.empty((m, d), dtype=h.dtype, device=h.device), d
+        else:
+            if h_out.dtype != h.dtype:
+                raise TypeError(f"h_out has type {h_out.dtype}, h {h.dtype}")
+            ldho = _rows(h_out, "h_out", m, d, index)
+        ldx = d
         if gamma_pre is None:
-            x, ldx = None, d
+            x = None
         elif x is None:
-            x, ldx = torch.empty((m, d), dtype=torch.bfloat16, device=dev), d
+            x = torch.empty((m, d), dtype=torch.bfloat16, device=h.device)
         else:
             if _dtype(x, "x") != IN_BF16:
                 raise TypeError("x must be bfloat16")
-            ldx = _rows(x, "x", m, d, dev)
-        rstd = torch.empty((2, m), dtype=torch.float32, device=dev) if save else None
-        rc = resq_block_norm_fwd(h.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, eps,
-                                 h_out.data_ptr(), ldho, _p(x), ldx, _p(rstd), s)
+            ldx = _rows(x, "x", m, d, index)
+        rstd = torch.empty((2, m), dtype=torch.float32, device=h.device) if save else None
+        rc = lib.resq_block_norm_fwd(h.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, eps,
+                                     h_out.data_ptr(), ldho, _p(x), ldx, _p(rstd), s)
+    finally:
+        if ctx is not None:
+            ctx.__exit__(None, None, None)
     _check(rc, "resq_block_norm_fwd")
     return h_out, x, rstd
 
@@ -723,36 +737,36 @@ def block_norm_bwd(h_out, rstd, dx=None, dh=None, y=None, gamma_post=None, gate=
     """Gradients of block_norm: dx and dh are those of its x and h_out (None: zero; dx goes with
     gamma_pre), the other arguments the forward's and rstd its output.  Returns a dict of dh (of
     h), dy (`out` type), dgamma_post, dgamma_pre and dgate (float32; None where there is none)."""
-    import torch
-    if h_out.dim() != 2:
-        raise ValueError("h_out must be a matrix")
-    m, d = h_out.shape
+    torch, lib = _th(), load()
+    m, d, index = _matrix(h_out, "h_out")
     dev = h_out.device
-    bits = (torch.bfloat16, torch.int16, torch.uint16)
-    hd, ldh = _dtype(h_out, "h_out"), _rows(h_out, "h_out", m, d, dev)
-    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, dev))
-    xd, lddx = (IN_BF16, d) if dx is None else (_dtype(dx, "dx"), _rows(dx, "dx", m, d, dev))
+    hd, ldh = _dtype(h_out, "h_out"), _rows(h_out, "h_out", m, d, index)
+    yd, ldy = (IN_BF16, d) if y is None else (_dtype(y, "y"), _rows(y, "y", m, d, index))
+    xd, lddx = (IN_BF16, d) if dx is None else (_dtype(dx, "dx"), _rows(dx, "dx", m, d, index))
     lddho = d
     if dh is not None:
         if _dtype(dh, "dh") != hd:
             raise TypeError(f"dh has type {dh.dtype}, h_out {h_out.dtype}")
-        lddho = _rows(dh, "dh", m, d, dev)
-    g, gd, gm = _gate_args(gate, m, d, dev)
-    gpost, gpre = _vector(gamma_post, "gamma_post", d, bits, dev), _vector(gamma_pre, "gamma_pre", d, bits, dev)
-    rs = _vector(rstd, "rstd", 2 * m, (torch.float32,), dev)
+        lddho = _rows(dh, "dh", m, d, index)
+    g, gd, gm = _gate_args(gate, m, d, index)
+    gpost, gpre = _vector(gamma_post, "gamma_post", d, IN_BF16, index), _vector(gamma_pre, "gamma_pre", d, IN_BF16, index)
+    rs = _vector(rstd, "rstd", 2 * m, IN_F32, index)
     yt = _out_code(out)
-    with _On(h_out, stream) as s:
-        def empty(*shape, dtype=torch.float32):
-            return torch.empty(shape, dtype=dtype, device=dev)
-        r = {"dh": empty(m, d, dtype=_like(hd)) if want_dh else None,
-             "dy": empty(m, d, dtype=_like(yt)) if want_dy else None,
-             "dgamma_post": empty(d) if gamma_post is not None else None,
-             "dgamma_pre": empty(d) if gamma_pre is not None else None,
-             "dgate": None if gate is None else empty(*gate.shape)}
-        keep, wp, nb = _ws_arg(ws, OP_BLOCK_NORM_BWD, m, d, 0, dev)
-        rc = resq_block_norm_bwd(h_out.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, rs,
-                                 _p(dx), xd, lddx, _p(dh), lddho, _p(r["dh"]), d, _p(r["dy"]), yt, d,
-                                 _p(r["dgamma_post"]), _p(r["dgamma_pre"]), _p(r["dgate"]), wp, nb, s)
+    ctx, s = _enter(index, stream)
+    try:
+        f32, empty = torch.float32, torch.empty
+        r = {"dh": empty((m, d), dtype=_TYPES[hd], device=dev) if want_dh else None,
+             "dy": empty((m, d), dtype=_TYPES[yt], device=dev) if want_dy else None,
+             "dgamma_post": empty(d, dtype=f32, device=dev) if gamma_post is not None else None,
+             "dgamma_pre": empty(d, dtype=f32, device=dev) if gamma_pre is not None else None,
+             "dgate": None if gate is None else empty(gate.shape, dtype=f32, device=dev)}
+        keep, wp, nb = _ws_arg(lib, ws, OP_BLOCK_NORM_BWD, m, d, 0, dev)
+        rc = lib.resq_block_norm_bwd(h_out.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre,
+                                     rs, _p(dx), xd, lddx, _p(dh), lddho, _p(r["dh"]), d, _p(r["dy"]), yt, d,
+                                     _p(r["dgamma_post"]), _p(r["dgamma_pre"]), _p(r["dgate"]), wp, nb, s)
+    finally:
+        if ctx is not None:
+            ctx.__exit__(None, None, None)
     _check(rc, "resq_block_norm_bwd")
     return r
 
@@ -760,31 +774,33 @@ def block_norm_bwd(h_out, rstd, dx=None, dh=None, y=None, gamma_post=None, gate=
 def matvec_w4a16(x, qw_codes, qw_scales, fmt, out="f32", y=None, stream=None):
     """Y = X Q(W)^T for at most MATVEC_MAX_ROWS rows of bfloat16 x (linear_w4a16 for more): float32,
     or with out="bf16" rounded to bfloat16."""
-    import torch
+    torch, lib = _th(), load()
     f = _fmt(fmt)
-    if x.dim() != 2 or qw_codes.dim() != 2:
-        raise ValueError("x and qw_codes must be matrices")
-    m, d = x.shape
-    n = qw_codes.shape[0]
-    dev = x.device
+    m, d, index = _matrix(x, "x")
+    n, half, _ = _matrix(qw_codes, "qw_codes")
     if _dtype(x, "x") != IN_BF16:
         raise TypeError("x must be bfloat16")
-    ldx = _rows(x, "x", m, d, dev)
-    if qw_codes.shape[1] * 2 != d:
-        raise ValueError(f"qw_codes hold rows of {qw_codes.shape[1] * 2}, x of {d}")
-    shape, _ = scale_shape(f, n, d)
-    cp = _vector(qw_codes, "qw_codes", n * (d // 2), (torch.uint8,), dev)
-    sp = _vector(qw_scales, "qw_scales", shape[0] * shape[1],
-                 (torch.uint8,) if f == MXFP4 else (torch.int32, torch.uint32), dev)
+    ldx = _rows(x, "x", m, d, index)
+    if half * 2 != d:
+        raise ValueError(f"qw_codes hold rows of {half * 2}, x of {d}")
+    cp = _vector(qw_codes, "qw_codes", n * half, torch.uint8, index)
+    if f == MXFP4:
+        sp = _vector(qw_scales, "qw_scales", n * (d // 32), torch.uint8, index)
+    else:
+        sp = _vector(qw_scales, "qw_scales", n * (d // 64), torch.uint32 if qw_scales.dtype == torch.uint32 else torch.int32, index)
     yt = _out_code(out)
-    with _On(x, stream) as s:
+    ctx, s = _enter(index, stream)
+    try:
         if y is None:
-            y, ldy = torch.empty((m, n), dtype=_like(yt), device=dev), n
+            y, ldy = torch.empty((m, n), dtype=_TYPES[yt], device=x.device), n
         else:
             if _dtype(y, "y") != yt:
                 raise TypeError(f"y has type {y.dtype}, out is {out!r}")
-            ldy = _rows(y, "y", m, n, dev)
-        rc = resq_matvec_w4a16(f, x.data_ptr(), m, d, ldx, cp, sp, n, y.data_ptr(), yt, ldy, s)
+            ldy = _rows(y, "y", m, n, index)
+        rc = lib.resq_matvec_w4a16(f, x.data_ptr(), m, d, ldx, cp, sp, n, y.data_ptr(), yt, ldy, s)
+    finally:
+        if ctx is not None:
+            ctx.__exit__(None, None, None)
     _check(rc, "resq_matvec_w4a16")
     return y
 
@@ -794,23 +810,30 @@ def token_logprobs(logits, targets=None, temperature=1.0, top_k=0, ws=None, stre
     (float32 or bfloat16) at a temperature.  Returns a dict: logp (m; with targets), stats (m x 3:
     the largest logit, log sum exp relative to it, the entropy) and, with top_k, top_logp and
     top_index (m x top_k, int32)."""
-    import torch
-    if logits.dim() != 2:
-        raise ValueError("logits must be a matrix")
-    m, v = logits.shape
+    torch, lib = _th(), load()
+    m, v, index = _matrix(logits, "logits")
     dev = logits.device
-    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, dev)
-    tp = _vector(targets, "targets", m, (torch.int64,), dev)
+    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, index)
+    tp = _vector(targets, "targets", m, torch.int64, index)
     top_k = int(top_k)
-    with _On(logits, stream) as s:
-        r = {} if targets is None else {"logp": torch.empty(m, dtype=torch.float32, device=dev)}
-        r["stats"] = torch.empty((m, 3), dtype=torch.float32, device=dev)
+    ctx, s = _enter(index, stream)
+    try:
+        f32, empty = torch.float32, torch.empty
+        r, lp, tv, ti = {}, 0, 0, 0
+        if targets is not None:
+            r["logp"] = empty(m, dtype=f32, device=dev)
+            lp = r["logp"].data_ptr()
+        r["stats"] = empty((m, 3), dtype=f32, device=dev)
         if top_k > 0:
-            r["top_logp"] = torch.empty((m, top_k), dtype=torch.float32, device=dev)
-            r["top_index"] = torch.empty((m, top_k), dtype=torch.int32, device=dev)
-        keep, wp, nb = _ws_arg(ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
-        rc = resq_token_logprobs(logits.data_ptr(), dt, m, v, ld, tp, temperature, _p(r.get("logp")),
-                                 r["stats"].data_ptr(), top_k, _p(r.get("top_logp")), _p(r.get("top_index")), wp, nb, s)
+            r["top_logp"] = empty((m, top_k), dtype=f32, device=dev)
+            r["top_index"] = empty((m, top_k), dtype=torch.int32, device=dev)
+            tv, ti = r["top_logp"].data_ptr(), r["top_index"].data_ptr()
+        keep, wp, nb = _ws_arg(lib, ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
+        rc = lib.resq_token_logprobs(logits.data_ptr(), dt, m, v, ld, tp, temperature, lp, r["stats"].data_ptr(), top_k,
+                                     tv, ti, wp, nb, s)
+    finally:
+        if ctx is not None:
+            ctx.__exit__(None, None, None)
     _check(rc, "resq_token_logprobs")
     return r
 
@@ -820,24 +843,24 @@ def token_logprobs_bwd(logits, targets, stats, dlogp=None, dentropy=None, temper
     """The gradient of the logits from those of token_logprobs' logp (dlogp) and of the entropy
     stats[:, 2] (dentropy), either None for zero: m x V of type `out`.  stats is token_logprobs';
     dlogits may be logits (in place) when the types are equal."""
-    import torch
-    if logits.dim() != 2:
-        raise ValueError("logits must be a matrix")
-    m, v = logits.shape
-    dev = logits.device
-    f32 = (torch.float32,)
-    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, dev)
-    tp, st = _vector(targets, "targets", m, (torch.int64,), dev), _vector(stats, "stats", 3 * m, f32, dev)
-    da, db = _vector(dlogp, "dlogp", m, f32, dev), _vector(dentropy, "dentropy", m, f32, dev)
+    torch, lib = _th(), load()
+    m, v, index = _matrix(logits, "logits")
+    dt, ld = _dtype(logits, "logits"), _rows(logits, "logits", m, v, index)
+    tp, st = _vector(targets, "targets", m, torch.int64, index), _vector(stats, "stats", 3 * m, IN_F32, index)
+    da, db = _vector(dlogp, "dlogp", m, IN_F32, index), _vector(dentropy, "dentropy", m, IN_F32, index)
     ot = _out_code(out)
-    with _On(logits, stream) as s:
+    ctx, s = _enter(index, stream)
+    try:
         if dlogits is None:
-            dlogits, ldd = torch.empty((m, v), dtype=_like(ot), device=dev), v
+            dlogits, ldd = torch.empty((m, v), dtype=_TYPES[ot], device=logits.device), v
         else:
             if _dtype(dlogits, "dlogits") != ot:
                 raise TypeError(f"dlogits has type {dlogits.dtype}, out is {out!r}")
-            ldd = _rows(dlogits, "dlogits", m, v, dev)
-        rc = resq_token_logprobs_bwd(logits.data_ptr(), dt, m, v, ld, tp, temperature, st, da, db, dlogits.data_ptr(),
-                                     ot, ldd, s)
+            ldd = _rows(dlogits, "dlogits", m, v, index)
+        rc = lib.resq_token_logprobs_bwd(logits.data_ptr(), dt, m, v, ld, tp, temperature, st, da, db,
+                                         dlogits.data_ptr(), ot, ldd, s)
+    finally:
+        if ctx is not None:
+            ctx.__exit__(None, None, None)
     _check(rc, "resq_token_logprobs_bwd")
     return dlogits
