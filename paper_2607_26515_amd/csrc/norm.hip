@@ -79,7 +79,7 @@ __device__ __forceinline__ Place<E> place(int c, int L, int lane, int d) {
 }
 
 template <int E>
-__device__ __forceinline__ void load_gate(const void* gate, bool f32, int col, float g[E]) {
+__device__ __forceinline__ void load_gate(const void* gate, bool f32, uint32_t col, float g[E]) {
   if (f32) load_n<E>(reinterpret_cast<const float*>(gate) + col, g);
   else load_n<E>(reinterpret_cast<const uint16_t*>(gate) + col, g);
 }
@@ -90,7 +90,7 @@ __device__ __forceinline__ float token_gate(const void* gate, bool f32, int64_t 
 // What the branch is scaled by along its columns: alpha gamma_post, times a channel's gate.
 template <int E>
 __device__ __forceinline__ void branch_gain(const uint16_t* gamma_post, const void* gate, int gate_mode, bool gate_f32,
-                                            float alpha, int col, float w[E]) {
+                                            float alpha, uint32_t col, float w[E]) {
 #pragma unroll
   for (int i = 0; i < E; ++i) w[i] = alpha;
   float g[E];
@@ -220,42 +220,68 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
   const int sub = row_in_block<WAVES>(L), lane = threadIdx.x - sub * L, d = (int)p.d, groups = blockDim.x / L;
   const int64_t group = (int64_t)blockIdx.x * groups + sub, n_groups = (int64_t)gridDim.x * groups;
   const bool pre = p.gamma_pre != nullptr, post = p.gamma_post != nullptr, need_y = p.y != nullptr;
-  Place<E> at[C];
+  // Where group c lies.  With several, worked out at each use: kept, places and the addresses the
+  // compiler makes of them would be some 60 registers, and with them the row would not fit.
+  auto where = [&](int c) {
+    int l = lane;
+    if constexpr (C > 1) asm("" : "+v"(l));
+    return place<E>(c, L, l, d);
+  };
+  // Column sums: in registers for one group per lane, in LDS for more (each lane adds to its own).  With
+  // them in registers too, rows longer than 8192 had to be read a second time after the row sums: 1792 x
+  // 16384 took 194 us (bf16 h) and 256 us (float32) instead of 153 and 229.
+  constexpr bool kWide = C > 1;
+  extern __shared__ __attribute__((aligned(16))) uint8_t column_lds[];
+  f32x4* sums = reinterpret_cast<f32x4*>(column_lds) + threadIdx.x;  // [pre, branch][C][E / 4][1024]
+  float s_pre[E] = {}, s_branch[E] = {};
+  auto add_columns = [&](float (&regs)[E], int which, int c, const float (&v)[E]) {
+    if constexpr (kWide) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) at[c] = place<E>(c, L, lane, d);
-  float s_pre[C][E] = {}, s_branch[C][E] = {};
-  float hn[E], dx[E], e[E], yn[E];  // of one group; e starts as dh', yn as y
-  float kept[E];  // C > 1: dh' of a group that was moved back (its neighbour may store to it)
-  Raw<TH, E> raw_h, raw_e;
-  Raw<TX, E> raw_x;
-  Raw<TY, E> raw_y;
+      for (int i = 0; i < E / 4; ++i) {
+        f32x4& slot = sums[((which * C + c) * (E / 4) + i) * 1024];
+        slot = slot + f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) regs[i] += v[i];
+    }
+  };
+  if constexpr (kWide)
+    for (int i = 0; i < 2 * C * (E / 4); ++i) sums[i * 1024] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Raw<TH, E> raw_h[C], raw_e[C];
+  Raw<TX, E> raw_x[C];
+  Raw<TY, E> raw_y[C];
   Raw<uint16_t, E> raw_pre;
   float w[E];
-  auto gains = [&](int col) {
+  auto gain_pre = [&](uint32_t col) {
     if (pre) load_raw(p.gamma_pre + col, raw_pre);
-    branch_gain<E>(p.gamma_post, p.gate, p.gate_mode, p.gate_f32, p.alpha, col, w);
   };
-  auto fetch = [&](int64_t row, int col) {
-    if (pre) {
-      load_raw(reinterpret_cast<const TH*>(p.h) + row * p.ldh + col, raw_h);
-      load_raw(reinterpret_cast<const TX*>(p.dx) + row * p.lddx + col, raw_x);
+  auto gain_branch = [&](uint32_t col) { branch_gain<E>(p.gamma_post, p.gate, p.gate_mode, p.gate_f32, p.alpha, col, w); };
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint32_t col = where(c).col;
+      if (pre) {
+        load_raw(reinterpret_cast<const TH*>(p.h) + row * p.ldh + col, raw_h[c]);
+        load_raw(reinterpret_cast<const TX*>(p.dx) + row * p.lddx + col, raw_x[c]);
+      }
+      if (p.dho) load_raw(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col, raw_e[c]);
+      if (need_y) load_raw(reinterpret_cast<const TY*>(p.y) + row * p.ldy + col, raw_y[c]);
     }
-    if (p.dho) load_raw(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col, raw_e);
-    if (need_y) load_raw(reinterpret_cast<const TY*>(p.y) + row * p.ldy + col, raw_y);
   };
-  auto take = [&](float rh, float ry) {
+  auto take = [&](int c, float rh, float ry, float hn[E], float dx[E], float e[E], float yn[E]) {
     if (pre) {
-      unpack(raw_h, hn);
-      unpack(raw_x, dx);
+      unpack(raw_h[c], hn);
+      unpack(raw_x[c], dx);
 #pragma unroll
       for (int i = 0; i < E; ++i) hn[i] *= rh;
     }
-    if (p.dho) unpack(raw_e, e);
+    if (p.dho) unpack(raw_e[c], e);
     else
 #pragma unroll
       for (int i = 0; i < E; ++i) e[i] = 0.f;
     if (need_y) {
-      unpack(raw_y, yn);
+      unpack(raw_y[c], yn);
 #pragma unroll
       for (int i = 0; i < E; ++i) yn[i] *= ry;
     }
@@ -270,47 +296,46 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
     if (p.gate_mode == kGateToken) next_gt = token_gate(p.gate, p.gate_f32, row);
   };
   fetch_factors(min(group, p.m - 1));
-  if constexpr (C == 1) {
-    gains(at[0].col);
-    fetch(min(group, p.m - 1), at[0].col);
+  fetch(min(group, p.m - 1));
+  if constexpr (!kWide) {
+    gain_pre(where(0).col);
+    gain_branch(where(0).col);
   }
   for (int64_t k = 0; k < trips; ++k) {  // the same count for every lane: row_sum has a barrier
     const int64_t row = group + k * n_groups, next = min(row + n_groups, p.m - 1);
     const bool in = row < p.m;
     const float rh = next_rh, ry = next_ry, gt = next_gt;
     float s[3] = {0.f, 0.f, 0.f};
+    float hn[C][E], dx[E], e[C][E], yn[C][E];  // e starts as dh', yn as y
     if (in) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int col = at[c].col;
-        if constexpr (C > 1) {
-          __builtin_amdgcn_sched_barrier(0);  // one group's loads at a time: two do not fit the registers
-          gains(col);
-          fetch(row, col);
+        const Place<E> at = where(c);
+        if constexpr (kWide) {
+          __builtin_amdgcn_sched_barrier(0);
+          gain_pre(at.col);
+          gain_branch(at.col);
         }
-        take(rh, ry);
-        if constexpr (C == 1) fetch(next, col);
-        if constexpr (C > 1)
-          if (at[c].skip > 0)
-#pragma unroll
-            for (int i = 0; i < E; ++i) kept[i] = e[i];
+        take(c, rh, ry, hn[c], dx, e[c], yn[c]);
+        if constexpr (!kWide) fetch(next);
         if (pre) {
-          float g[E];
+          float g[E], x[E];
           unpack(raw_pre, g);
 #pragma unroll
           for (int i = 0; i < E; ++i) {
-            if constexpr (C == 1) s_pre[c][i] = fmaf(dx[i], hn[i], s_pre[c][i]);
+            x[i] = dx[i] * hn[c][i];
             const float u = dx[i] * g[i];
-            s[0] = fmaf(u, i >= at[c].skip ? hn[i] : 0.f, s[0]);
-            e[i] = fmaf(rh, u, e[i]);
+            s[0] = fmaf(u, i >= at.skip ? hn[c][i] : 0.f, s[0]);
+            e[c][i] = fmaf(rh, u, e[c][i]);
           }
+          add_columns(s_pre, 0, c, x);
         }
         if (need_y)
 #pragma unroll
           for (int i = 0; i < E; ++i) {
-            const float wy = i >= at[c].skip ? w[i] * yn[i] : 0.f;
-            s[1] = fmaf(wy, e[i], s[1]);
-            if (pre) s[2] = fmaf(wy, hn[i], s[2]);
+            const float wy = i >= at.skip ? w[i] * yn[c][i] : 0.f;
+            s[1] = fmaf(wy, e[c][i], s[1]);
+            if (pre) s[2] = fmaf(wy, hn[c][i], s[2]);
           }
       }
     }
@@ -323,79 +348,79 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
     const float km = we * gt / (float)d;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = at[c].col;
-      const bool mine = at[c].skip < E;
-      if constexpr (C > 1) {
-        __builtin_amdgcn_sched_barrier(0);  // two groups do not stay in registers beside the column sums
-        gains(col);
-        fetch(row, col);
-        take(rh, ry);
-        if (at[c].skip > 0)
-#pragma unroll
-          for (int i = 0; i < E; ++i) e[i] = kept[i];
-        if (pre) {
-          float g[E];
-          unpack(raw_pre, g);
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            s_pre[c][i] = fmaf(dx[i], hn[i], s_pre[c][i]);
-            e[i] = fmaf(rh, dx[i] * g[i], e[i]);
-          }
-        }
+      const Place<E> at = where(c);
+      const uint32_t col = at.col;
+      const bool mine = at.skip < E;
+      if constexpr (kWide) {
+        __builtin_amdgcn_sched_barrier(0);
+        gain_branch(col);
       }
       if (pre)
 #pragma unroll
-        for (int i = 0; i < E; ++i) e[i] = fmaf(-rc, hn[i], e[i]);
-      if (p.dh && mine) {
-        TH* dst = reinterpret_cast<TH*>(p.dh) + row * p.lddh + col;
-        if (C > 1 && at[c].skip > 0) {  // its neighbour may still have to read dh' there
+        for (int i = 0; i < E; ++i) e[c][i] = fmaf(-rc, hn[c][i], e[c][i]);
+      if (p.dh && mine) store_n<E>(reinterpret_cast<TH*>(p.dh) + row * p.lddh + col, e[c]);
+      if (need_y) {
+        float x[E];
 #pragma unroll
-          for (int i = 0; i < E; ++i)
-            if (i >= at[c].skip) store1(dst + i, e[i]);
-        } else {
-          store_n<E>(dst, e);
-        }
+        for (int i = 0; i < E; ++i) x[i] = gt * e[c][i] * yn[c][i];
+        add_columns(s_branch, 1, c, x);
       }
-      if (need_y)
-#pragma unroll
-        for (int i = 0; i < E; ++i) s_branch[c][i] = fmaf(gt * e[i], yn[i], s_branch[c][i]);
       if (p.dy && mine) {
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          e[i] *= gt * w[i];
-          if (post) e[i] = ry * (e[i] - yn[i] * km);
+          e[c][i] *= gt * w[i];
+          if (post) e[c][i] = ry * (e[c][i] - yn[c][i] * km);
         }
-        if (p.dy_f32) store_n<E>(reinterpret_cast<float*>(p.dy) + row * p.lddy + col, e);
-        else store_n<E>(reinterpret_cast<uint16_t*>(p.dy) + row * p.lddy + col, e);
+        if (p.dy_f32) store_n<E>(reinterpret_cast<float*>(p.dy) + row * p.lddy + col, e[c]);
+        else store_n<E>(reinterpret_cast<uint16_t*>(p.dy) + row * p.lddy + col, e[c]);
       }
+    }
+    if constexpr (kWide) {
+      __builtin_amdgcn_sched_barrier(0);
+      fetch(next);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // The workgroup's partial sums, [gridDim.x][d] each: row groups of one wave are added by lane
   // exchange, those of its four waves through LDS in wave order.
-  auto put = [&](float* part, float (&v)[C][E]) {
+  auto put = [&](float* part, float (&v)[E], int which) {
     if (part == nullptr) return;  // uniform
+    float* out = part + (int64_t)blockIdx.x * p.d;
+    if constexpr (kWide) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+          const f32x4 q = sums[((which * C + c) * (E / 4) + i / 4) * 1024];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[i + j] = q[j];
+        }
+        const Place<E> at = where(c);
+        if (at.skip < E) store_n<E>(out + at.col, v);
+      }
+      return;
+    }
     if (L <= 64) {
       __shared__ float rows[4][64 * E];
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        for (int o = L; o < 64; o <<= 1) v[0][i] += __shfl_xor(v[0][i], o, 64);
-        rows[threadIdx.x >> 6][(threadIdx.x & 63) * E + i] = v[0][i];
+        for (int o = L; o < 64; o <<= 1) v[i] += __shfl_xor(v[i], o, 64);
+        rows[threadIdx.x >> 6][(threadIdx.x & 63) * E + i] = v[i];
       }
       __syncthreads();
       if ((int)threadIdx.x < L)
 #pragma unroll
         for (int i = 0; i < E; ++i)
-          v[0][i] = (rows[0][threadIdx.x * E + i] + rows[1][threadIdx.x * E + i]) +
-                    (rows[2][threadIdx.x * E + i] + rows[3][threadIdx.x * E + i]);
+          v[i] = (rows[0][threadIdx.x * E + i] + rows[1][threadIdx.x * E + i]) +
+                 (rows[2][threadIdx.x * E + i] + rows[3][threadIdx.x * E + i]);
       __syncthreads();
       if ((int)threadIdx.x >= L) return;
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (at[c].skip < E) store_n<E>(part + (int64_t)blockIdx.x * p.d + at[c].col, v[c]);
+    const Place<E> at = where(0);
+    if (at.skip < E) store_n<E>(out + at.col, v);
   };
-  put(p.part_pre, s_pre);
-  put(p.part_branch, s_branch);
+  put(p.part_pre, s_pre, 0);
+  put(p.part_branch, s_branch, 1);
 }
 
 struct ColumnSums {
@@ -465,7 +490,7 @@ RowLanes row_lanes(int64_t d) {
 int64_t bwd_workgroups(int64_t m, int64_t d) {
   const RowLanes r = row_lanes(d);
   const int64_t rows = r.threads / r.L;
-  return std::min<int64_t>((m + rows - 1) / rows, 512);
+  return std::min<int64_t>((m + rows - 1) / rows, r.wide ? 256 : 512);
 }
 
 }  // namespace
@@ -510,7 +535,8 @@ void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgam
   if (q.dgamma_post || q.dgate) q.part[1] = p.part_branch = workspace + wgs * p.d;
   const int nv = (q.part[0] ? 1 : 0) + (q.part[1] ? 1 : 0);
   const dim3 grid((unsigned)wgs), block(r.threads);
-#define RESQ_NB(H, Y, X, E, C, W) launch_timed(norm_bwd_kernel<H, Y, X, E, C, W>, grid, block, 0u, s, p, r.L)
+  const uint32_t column_lds = r.wide ? 2 * 16 * 4 * 1024 : 0;  // two column sums, sixteen a lane
+#define RESQ_NB(H, Y, X, E, C, W) launch_timed(norm_bwd_kernel<H, Y, X, E, C, W>, grid, block, column_lds, s, p, r.L)
 #define RESQ_NB2(H, Y, X)                             \
   do {                                                \
     if (r.one) RESQ_NB(H, Y, X, 1, 1, false);         \
