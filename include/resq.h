@@ -331,11 +331,13 @@ int resq_linear_w16a4(int format, const uint16_t* X, int64_t m, int64_t d, int64
  * resq_matvec_w4a16 - resq_linear_w4a16 for the few tokens of a rollout's tail: Y = X Q(W)^T for
  * m <= 16 rows (RESQ_ERR_UNSUPPORTED beyond), bound by one read of Q(W).
  * X: m x d bf16, any row stride ldx >= d, 2-byte aligned.  Q(W): K-major codes and scales as for
- *   resq_linear_w4a16 (codes 16-byte, HiF4 scales 4-byte aligned).  d: a multiple of the block.
+ *   resq_linear_w4a16 (codes 16-byte, HiF4 scales 4-byte aligned).  d: a multiple of the block, at
+ *   most 56832 (RESQ_ERR_UNSUPPORTED beyond).
  * Y: m x n, row stride ldy >= n, float32 (y_dtype = RESQ_IN_F32) or bf16 (RESQ_IN_BF16: the
  *   float32 result rounded once, ties to even).  d = 0 writes zeros.
- * Products are exact; the sum over d is float32, in an order fixed by the sizes.  Sums may
- * therefore differ from resq_linear_w4a16's in their last bits.  No workspace.
+ * Products are exact; the sum over d is float32, in an order fixed by n and d: a token's result is
+ * the same alone and among others, and may differ from resq_linear_w4a16's in its last bits.
+ * No workspace.
  */
 int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64_t ldx,
                       const uint8_t* qw_codes, const void* qw_scales, int64_t n, void* Y, int y_dtype,
@@ -361,7 +363,8 @@ int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64
  * rstd     : 2 x m float32 outputs, r_post then r_pre (0 for an absent norm), which the backward
  *            reads; NULL to skip.
  * Pointers are aligned to their elements; every row stride >= d.  d <= 16384 and m < 2^31
- * (RESQ_ERR_UNSUPPORTED beyond).  Apart from H_out = H, outputs overlap no input.  No workspace.
+ * (RESQ_ERR_UNSUPPORTED beyond).  Apart from H_out = H, outputs overlap no
+ * input and no other output (here and below).  No workspace.
  *
  * resq_block_norm_bwd - the gradients, given those of X (dX, of dx_dtype: resq_linear_bwd's
  * float32 dX, or bf16) and of H' (dH_out, of h_dtype; NULL: zero):

@@ -315,6 +315,7 @@ int check_logits(const void* logits, int dtype, int64_t m, int64_t V, int64_t ld
   if (m < 0 || V < 0) return fail(RESQ_ERR_ARG, "negative size (m=%lld, V=%lld)", (long long)m, (long long)V);
   if (V == 0 && m > 0) return fail(RESQ_ERR_SHAPE, "rows of no logits (V=0)");
   if (V > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "V (%lld) must be below 2^31", (long long)V);
+  if (m > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "m (%lld) must be below 2^31", (long long)m);
   if (!(temperature >= 0x1p-64 && temperature <= 0x1p64))
     return fail(RESQ_ERR_ARG, "temperature (%g) must lie in [2^-64, 2^64]", temperature);
   if ((uintptr_t)targets % 8 != 0) return fail(RESQ_ERR_ARG, "targets must be 8-byte aligned");
@@ -943,7 +944,6 @@ int resq_token_logprobs(const void* logits, int dtype, int64_t m, int64_t V, int
   if (rc != RESQ_OK) return rc;
   if (top_k < 0 || top_k > resq::kMaxTop)
     return fail(RESQ_ERR_ARG, "top_k (%d) must lie in 0..%d", top_k, resq::kMaxTop);
-  if (m > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "m (%lld) must be below 2^31", (long long)m);
   if (m == 0) return ok();
   if (logp && !targets) return fail(RESQ_ERR_ARG, "logp without targets");
   if (!stats) return fail(RESQ_ERR_ARG, "stats is NULL");
@@ -972,7 +972,6 @@ int resq_token_logprobs_bwd(const void* logits, int dtype, int64_t m, int64_t V,
   if (!targets || !stats) return fail(RESQ_ERR_ARG, "targets / stats is NULL");
   if ((uintptr_t)stats % 4 != 0 || (uintptr_t)dlogp % 4 != 0 || (uintptr_t)dentropy % 4 != 0)
     return fail(RESQ_ERR_ARG, "stats, dlogp and dentropy must be 4-byte aligned");
-  if (!resq::logprob_bwd_supported(m, V)) return fail(RESQ_ERR_UNSUPPORTED, "m * V too large for one launch");
   const resq::LogprobBwd p{logits, m, V, ld, targets, temperature, stats, dlogp, dentropy, dlogits, ldd};
   const hipStream_t s = (hipStream_t)stream;
   {

@@ -242,7 +242,6 @@ struct LogprobBwd {
   void* dlogits;
   int64_t ldd;
 };
-bool logprob_bwd_supported(int64_t m, int64_t V);  // the grid fits a launch
 void launch_logprob_bwd(const LogprobBwd& p, bool f32, bool out_f32, hipStream_t s);
 
 // Activation statistics (diag.hip): stats receives 9 doubles (see resq_diagnostics);

@@ -176,6 +176,13 @@ __device__ __forceinline__ Sums wave_join(const Sums& a, float c, int lane) {
   return {s.M, wave_sum(s.S, lane), wave_sum(s.W, lane)};
 }
 
+// Rows lie along y and z of a grid: a dimension holds less than 2^32 threads, and y and z 65535 workgroups.
+constexpr int64_t kGridRows = 32768;
+dim3 row_grid(int64_t x, int64_t rows) {
+  return dim3((unsigned)x, (unsigned)std::min(rows, kGridRows), (unsigned)((rows + kGridRows - 1) / kGridRows));
+}
+__device__ __forceinline__ int64_t grid_row() { return (int64_t)blockIdx.z * gridDim.y + blockIdx.y; }
+
 struct Args {
   LogprobFwd p;
   float c, inv_t;       // log2(e) / T, 1 / T
@@ -224,7 +231,8 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
   __shared__ Sums wave_sums[W];
   __shared__ uint64_t maxima[TOP ? 64 : 1], lists[TOP ? W / 2 : 1][32], joined[TOP ? 32 : 1], found[TOP ? W : 1][128];
   __shared__ int counts[W];
-  const int64_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const int64_t row = grid_row(), split = blockIdx.x;
+  if (row >= a.p.m) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool dead = a.p.targets && a.p.targets[row] < 0;
   if (dead && a.splits > 1) return;
@@ -355,8 +363,8 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
   if (a.splits == 1) {
     finish<T>(a, row, s, list, lane);
   } else {
-    if (lane == 0) a.sums[blockIdx.x] = s;
-    if (TOP && lane < 32) a.keys[(int64_t)blockIdx.x * 32 + lane] = list;
+    if (lane == 0) a.sums[row * a.splits + split] = s;
+    if (TOP && lane < 32) a.keys[(row * a.splits + split) * 32 + lane] = list;
   }
 }
 
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
 constexpr int kJoinWaves = 8;
 template <typename T, bool TOP>
 __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(Args a) {
-  const int64_t row = blockIdx.x;
+  const int64_t row = blockIdx.x;  // splits are for few rows
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool dead = a.p.targets && a.p.targets[row] < 0;
   uint64_t list = 0ull;
@@ -406,9 +414,10 @@ constexpr int kBwdThreads = 256;
 constexpr int64_t kBwdLen = (int64_t)kBwdThreads * 8 * 2;
 
 template <typename T, typename O>
-__global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwd p, int64_t parts, float inv_t) {
-  const int64_t row = blockIdx.x / parts;
-  const int64_t lo = (blockIdx.x % parts) * kBwdLen, hi = min(p.V, lo + kBwdLen);
+__global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwd p, float inv_t) {
+  const int64_t row = grid_row();
+  if (row >= p.m) return;
+  const int64_t lo = blockIdx.x * kBwdLen, hi = min(p.V, lo + kBwdLen);
   const T* x = reinterpret_cast<const T*>(p.logits) + row * p.ld;
   O* out = reinterpret_cast<O*>(p.dlogits) + row * p.ldd;
   const int64_t target = p.targets[row];
@@ -455,7 +464,7 @@ void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStrea
   a.len = split_len(p.V, a.splits);
   a.sums = (Sums*)workspace;
   a.keys = (uint64_t*)((char*)workspace + up256((size_t)(p.m * a.splits) * sizeof(Sums)));
-  const dim3 grid((unsigned)(p.m * a.splits)), joins((unsigned)p.m);
+  const dim3 grid = row_grid(a.splits, p.m), joins((unsigned)p.m);
 #define RESQ_LP(T, K)                                                                          \
   do {                                                                                         \
     if (waves_for(p.V) == 2) launch_timed(logprob_kernel<T, K, 2>, grid, dim3(128), 0u, s, a); \
@@ -467,15 +476,10 @@ void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStrea
 #undef RESQ_LP
 }
 
-bool logprob_bwd_supported(int64_t m, int64_t V) {
-  return m <= INT32_MAX / std::max<int64_t>(1, (V + kBwdLen - 1) / kBwdLen);
-}
-
 void launch_logprob_bwd(const LogprobBwd& p, bool f32, bool out_f32, hipStream_t s) {
-  const int64_t parts = (p.V + kBwdLen - 1) / kBwdLen;
-  const dim3 grid((unsigned)(p.m * parts));
+  const dim3 grid = row_grid((p.V + kBwdLen - 1) / kBwdLen, p.m);
   const float inv_t = (float)(1.0 / p.temperature);
-#define RESQ_LB(T, O) launch_timed(logprob_bwd_kernel<T, O>, grid, dim3(kBwdThreads), 0u, s, p, parts, inv_t)
+#define RESQ_LB(T, O) launch_timed(logprob_bwd_kernel<T, O>, grid, dim3(kBwdThreads), 0u, s, p, inv_t)
   if (f32) { if (out_f32) RESQ_LB(float, float); else RESQ_LB(float, uint16_t); }
   else { if (out_f32) RESQ_LB(uint16_t, float); else RESQ_LB(uint16_t, uint16_t); }
 #undef RESQ_LB

@@ -121,7 +121,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_kernel(NormFwd p, int L) {
     __syncthreads();
   }
   const int sub = row_in_block<WAVES>(L), lane = threadIdx.x - sub * L, d = (int)p.d;
-  const int64_t row0 = (int64_t)blockIdx.x * (blockDim.x / L) + sub, row = min(row0, p.m - 1);
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / L) + sub, row = min(row0, p.m - 1);
   const bool in = row0 < p.m;
   const bool first = in && lane == 0, post = p.gamma_post != nullptr, pre = p.gamma_pre != nullptr;
   Place<E> at[C];
@@ -502,8 +502,9 @@ size_t norm_bwd_ws_bytes(int64_t m, int64_t d) {
 
 void launch_norm_fwd(const NormFwd& p, bool h_f32, bool y_f32, hipStream_t s) {
   const RowLanes r = row_lanes(p.d);
-  const int64_t rows = r.threads / r.L;
-  const dim3 grid((unsigned)((p.m + rows - 1) / rows)), block(r.threads);
+  const int64_t rows = r.threads / r.L, groups = (p.m + rows - 1) / rows, most = 1 << 20;
+  // in two dimensions: one holds less than 2^32 threads
+  const dim3 grid((unsigned)std::min(groups, most), (unsigned)((groups + most - 1) / most)), block(r.threads);
 #define RESQ_NF(H, Y, E, C, W) launch_timed(norm_fwd_kernel<H, Y, E, C, W>, grid, block, 0u, s, p, r.L)
 #define RESQ_NF2(H, Y)                         \
   do {                                         \

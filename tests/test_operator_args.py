@@ -171,3 +171,13 @@ def test_refused_calls_keep_the_error_message_of_their_entry_point():
     assert lib is not None
     assert matvec(m=17) == B.ERR_UNSUPPORTED and "resq_linear_w4a16" in P.resq_last_error()
     assert fwd(Y=0) == B.ERR_ARG and "gamma_pre" in P.resq_last_error()
+
+
+def test_limits_of_lengths():
+    """The longest row of the few-token product, the longest norm, and one step past each."""
+    assert matvec(d=56832, ldx=56832, X=0) == B.ERR_ARG  # gets as far as the operands
+    assert matvec(d=56832 + 64, ldx=56832 + 64) == B.ERR_UNSUPPORTED
+    assert fwd(d=16384, ldh=16384, ldy=16384, ldho=16384, ldx=16384, H=0) == B.ERR_ARG
+    assert fwd(d=16385, ldh=16385, ldy=16385, ldho=16385, ldx=16385) == B.ERR_UNSUPPORTED
+    assert lp(m=1 << 31) == B.ERR_UNSUPPORTED and lpb(m=1 << 31) == B.ERR_UNSUPPORTED
+    assert fwd(m=1 << 31) == B.ERR_UNSUPPORTED and bwd(m=1 << 31) == B.ERR_UNSUPPORTED
