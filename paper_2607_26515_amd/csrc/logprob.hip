@@ -229,8 +229,12 @@ template <typename T, bool TOP, int W>
 __global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
   constexpr int kStep = 64 * W * kGroup, kTrip = kStep * kUnroll;
   __shared__ Sums wave_sums[W];
-  __shared__ uint64_t maxima[TOP ? 64 : 1], lists[TOP ? W / 2 : 1][32], joined[TOP ? 32 : 1], found[TOP ? W : 1][128];
-  __shared__ int counts[W];
+  constexpr int kPool = W > 4 ? 64 * W : 256;  // candidates that are ranked by counting
+  __shared__ uint64_t maxima[TOP ? W : 1][64], pool[TOP ? kPool : 2], lists[TOP ? W / 2 : 1][32], joined[TOP ? 32 : 1];
+  __shared__ uint64_t bound_lds;
+  __shared__ int n_pool;
+  __shared__ uint8_t owner_lanes[TOP ? W : 1][64];
+  __shared__ Sums row_sums;
   const int64_t row = grid_row(), split = blockIdx.x;
   if (row >= a.p.m) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -299,67 +303,97 @@ __global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
   s = wave_join(s, a.c, lane);
   if (lane == 0) wave_sums[wave] = s;
   [[maybe_unused]] uint64_t mine = 0ull;
-  if constexpr (TOP) {  // the largest keys of W lanes each
+  if constexpr (TOP) {
     mine = top_key(best, best_at);
-    uint64_t g = mine;
-    if constexpr (W >= 2) g = max(g, lane_xor<1>(g, lane));
-    if constexpr (W >= 4) g = max(g, lane_xor<2>(g, lane));
-    if constexpr (W >= 8) g = max(g, lane_xor<4>(g, lane));
-    if (lane % W == 0) maxima[tid / W] = g;
+    maxima[wave][lane] = mine;
+    if (tid < 32) joined[tid] = 0ull;
+    if (tid == 0) n_pool = 0;
   }
   __syncthreads();
-  if (wave == 0) s = wave_join(lane < W ? wave_sums[lane] : empty_sums(), a.c, lane);
+  if (wave == W - 1) {
+    s = wave_join(lane < W ? wave_sums[lane] : empty_sums(), a.c, lane);
+    if (lane == 0) row_sums = s;
+  }
   uint64_t list = 0ull;
   if constexpr (TOP) {
-    // The bound: the k-th largest of the 64 maxima.  As an element's key, the last index of the
-    // bounding group: no element of that group is below it.
-    const uint64_t last = __shfl(sort64(maxima[lane], lane), a.p.top_k - 1, 64);
-    const uint64_t bound = last == 0ull ? 1ull : last - 7;
-    // Every wave looks through the elements of its own lanes whose largest is not below.
-    int n_found = 0;
-    bool overflow = false;
-    auto consider = [&](uint64_t k) {
-      const uint64_t hit = __ballot(k >= bound);
-      if (k >= bound) found[wave][n_found + __popcll(hit & ((1ull << lane) - 1))] = k;
-      n_found += __popcll(hit);
-      if (n_found >= 64) {  // many near the bound: keep the largest 32
-        list = take64(list, found[wave][lane], lane);
-        overflow = true;
-        n_found -= 64;
-        if (lane < n_found) found[wave][lane] = found[wave][64 + lane];
+    // The bound: the k-th largest of the 64 maxima of W lanes each.  As an element's key, the last index
+    // of the bounding group: no element of that group is below it.
+    if (wave == 0) {
+      uint64_t g = mine;
+#pragma unroll
+      for (int w = 1; w < W; ++w) g = max(g, maxima[w][lane]);
+      g = sort64(g, lane);
+      if (lane == a.p.top_k - 1) bound_lds = g;
+    }
+    __syncthreads();
+    const uint64_t last = bound_lds, bound = last == 0ull ? 1ull : last - 7;
+    // Every wave looks through the elements of its own lanes whose largest is not below, eight groups (of
+    // one lane, or of several where a lane has few) to a load.
+    const bool owner = mine != 0ull && mine >= last;
+    const uint64_t owners = __ballot(owner), below = (1ull << lane) - 1;
+    const int n_owners = __popcll(owners);
+    if (owner) owner_lanes[wave][__popcll(owners & below)] = (uint8_t)lane;
+    const int groups = (int)((hi - lo + kStep - 1) / kStep), chunks = max(1, (groups + 7) / 8);
+    const int sh = groups > 4 ? 3 : groups > 2 ? 2 : groups > 1 ? 1 : 0;
+    const int own_at = (lane >> 3) >> sh, group_at = (lane >> 3) & ((1 << sh) - 1);
+    const bool has_head = split == 0 && wave == 0 && head > 0 && (owners & 1);
+    auto scan = [&](auto&& consider) {
+      if (has_head) consider(lane < head ? top_key(load1(x + lane), (uint32_t)lane) : 0ull);
+      int o = 0, c = 0;
+      while (o < n_owners) {
+        float v[4];
+        uint32_t idx[4];
+        bool ok[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int own = o + own_at, g = 8 * c + group_at;
+          const int64_t at = lo + (tid - lane + owner_lanes[wave][min(own, 63)]) * (int64_t)kGroup + (int64_t)g * kStep + lane % kGroup;
+          ok[u] = own < n_owners && g < groups && at < hi;
+          idx[u] = (uint32_t)at;
+          v[u] = load1(x + (ok[u] ? at : 0));
+          if (++c == chunks) {
+            c = 0;
+            o += 8 >> sh;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) consider(ok[u] ? top_key(v[u], idx[u]) : 0ull);
       }
     };
-    uint64_t owners = __ballot(mine != 0ull && mine >= last);
-    if (split == 0 && wave == 0 && head > 0 && (owners & 1))
-      consider(lane < head ? top_key(load1(x + lane), (uint32_t)lane) : 0ull);
-    for (; owners != 0ull; owners &= owners - 1) {
-      const int64_t first = lo + (int64_t)(tid - lane + __builtin_ctzll(owners)) * kGroup;
-      for (int64_t t0 = first; t0 < hi; t0 += 64 / kGroup * kStep) {  // eight groups at a time
-        const int64_t at = t0 + lane / kGroup * kStep + lane % kGroup;
-        consider(at < hi ? top_key(load1(x + at), (uint32_t)at) : 0ull);
-      }
-    }
-    if (lane == 0) counts[wave] = overflow ? -1 : n_found;
-    if (tid < 32) joined[tid] = 0ull;
+    scan([&](uint64_t k) {
+      const uint64_t hit = __ballot(k >= bound);
+      if (hit == 0ull) return;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&n_pool, __popcll(hit));
+      at = __builtin_amdgcn_readfirstlane(at) + __popcll(hit & below);
+      if (k >= bound && at < kPool) pool[at] = k;
+    });
     __syncthreads();
-    bool any = false;
-    for (int w = 0; w < W; ++w) any |= counts[w] < 0;
-    if (any) {
-      if (n_found > 0) list = take64(list, lane < n_found ? found[wave][lane] : 0ull, lane);
+    const int n = n_pool;
+    if (n > kPool) {  // many near the bound: every wave keeps its largest 32
+      uint64_t least = bound;
+      scan([&](uint64_t k) {
+        if (__ballot(k >= least) == 0ull) return;
+        list = take64(list, k >= least ? k : 0ull, lane);
+        least = max(least, (uint64_t)__shfl(list, 31, 64));
+      });
       list = join_lists<W>(list, lists, tid);
-    } else {  // the usual case, about k candidates: a key's place is the number of larger ones
-      if (lane < n_found) {
-        const uint64_t key = found[wave][lane];
+    } else {  // the usual case, about k: a key's place is the number of larger ones
+      for (int i = tid; i < n; i += 64 * W) {
+        const uint64_t key = pool[i];
         int place = 0;
-        for (int w = 0; w < W; ++w)
-          for (int i = 0; i < counts[w]; ++i) place += found[w][i] > key ? 1 : 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) place += pool[j] > key ? 1 : 0;
         if (place < 32) joined[place] = key;
       }
       __syncthreads();
       list = lane < 32 ? joined[lane] : 0ull;
     }
+  } else {
+    __syncthreads();
   }
   if (wave != 0) return;
+  s = row_sums;
   if (a.splits == 1) {
     finish<T>(a, row, s, list, lane);
   } else {
