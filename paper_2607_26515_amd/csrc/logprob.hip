@@ -226,7 +226,7 @@ __device__ __forceinline__ void finish(const Args& a, int64_t row, const Sums& s
 
 // One workgroup of W waves per row and split.
 template <typename T, bool TOP, int W>
-__global__ __launch_bounds__(64 * W) void logprob_kernel(Args a) {
+__global__ __launch_bounds__(64 * W, 8) void logprob_kernel(Args a) {
   constexpr int kStep = 64 * W * kGroup, kTrip = kStep * kUnroll;
   __shared__ Sums wave_sums[W];
   constexpr int kPool = W > 4 ? 64 * W : 256;  // candidates that are ranked by counting
