@@ -19,7 +19,7 @@
 // 2.3 a wave at 4 x 37888 x 3584, the same loop took 23.0 us instead of 22.0.)
 //
 // Data movement.  X lies in LDS.  Tokens that do not fit together are taken in B batches by B
-// workgroups on one XCD, each with B shares (so that X is copied once per workgroup and the codes come
+// workgroups on one XCD, each with up to B shares (so that X is copied once per workgroup and the codes come
 // from HBM once and from the L2 B - 1 times).  Codes and scales go straight into a ring of kAhead steps
 // in each wave's own part of LDS (buffer loads with the LDS destination: a step waits for its own loads
 // only; with loads to registers the compiler waited for all in flight).  Tokens past the last repeat
@@ -64,7 +64,7 @@ struct MatvecParams {
   int64_t ldy, n;
   int m, d;
   int batch, batches;     // tokens in LDS at a time
-  int shares, groups;     // shares of quads; workgroups per batch, a multiple of 8 (one XCD per share)
+  int shares, each, groups;  // shares of quads, of a workgroup; workgroups per batch, a multiple of 8 (one XCD per share)
   int quads, quads_left;  // quads per share; the first quads_left shares have one more
   int part_at, part_stride, part_flip;  // LDS of a wave's parts of quads; distance of two shares' (B > 1)
   bool out_bf16;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
   const int j = lane & 3, blk = lane >> 2;
   const int turns = (p.d + kStep - 1) / kStep;
   const int t0 = (int)(blockIdx.x / p.groups) * p.batch, tokens = min(p.batch, p.m - t0);  // may be none
-  const int share0 = (int)(blockIdx.x % p.groups) * p.batches, share1 = min(p.shares, share0 + p.batches);
+  const int share0 = (int)(blockIdx.x % p.groups) * p.each, share1 = min(p.shares, share0 + p.each);
   if (share0 >= share1 || tokens <= 0) return;
 
   // A share's steps, and those of a wave (parts that differ by one at most).
@@ -247,28 +247,25 @@ __global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
       }
     }
   };
-  // The 16 blocks' sums added: lane 4 r + j (r < 4) gets token r of row j.  Clears them.
+  // The 16 blocks' sums added, the four tokens' in one go: lane 16 r + j (j < 4) gets token r of row j.
+  // Clears them.
   auto reduce = [&](float out[TG]) {
 #pragma unroll
     for (int g = 0; g < TG; ++g) {
-      out[g] = 0.f;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float s = sum[g][r];
-        s += dpp<kDppRor8>(s);
-        s += dpp<kDppRor4>(s);
-        s = add_swapped<true>(add_swapped<false>(s));
-        if (blk == r) out[g] = s;
-        sum[g][r] = 0.f;
-      }
+      float v = add_pair<false>(add_pair<true>(sum[g][0], sum[g][2]), add_pair<true>(sum[g][1], sum[g][3]));
+      v += dpp<kDppRor8>(v);
+      out[g] = v + dpp<kDppRor4>(v);
+      sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
+  const bool holds = (blk & 3) == 0;  // this lane's sum is the one that is kept: of token 4 g + tok
+  const int tok = lane >> 4;
   auto store = [&](int quad, const float v[TG]) {
     const int64_t row = 4 * (int64_t)quad + j;
-    if (blk >= 4 || row >= p.n) return;
+    if (!holds || row >= p.n) return;
 #pragma unroll
     for (int g = 0; g < TG; ++g) {
-      const int tk = 4 * g + blk;
+      const int tk = 4 * g + tok;
       if (tk >= tokens) continue;
       const int64_t at = (int64_t)(t0 + tk) * p.ldy + row;
       if (p.out_bf16) reinterpret_cast<uint16_t*>(p.Y)[at] = bf16_bits(v[g]);
@@ -322,18 +319,18 @@ __global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
     reduce(tail);
     const bool inside = count > 0 && !whole;  // its only quad neither begins nor ends here
     const int at = p.part_at + ((sh - share0) & 1) * p.part_flip;
-    if (blk < 4)
+    if (holds)
 #pragma unroll
       for (int g = 0; g < TG; ++g)
-        reinterpret_cast<float*>(lds + at + wave * p.part_stride)[g * 16 + lane] = inside ? tail[g] : head[g];
+        reinterpret_cast<float*>(lds + at + wave * p.part_stride)[g * 16 + 4 * tok + j] = inside ? tail[g] : head[g];
     lds_barrier();
     if (whole && turn > 0) {  // this wave began the quad: add the waves after it up to the quad's end
       const uint32_t end = (uint32_t)(quad - q0 + 1) * turns;
       for (int v = wave + 1; v < kWaves && begin_of(sh, v) < end; ++v)
-        if (blk < 4 && begin_of(sh, v + 1) > begin_of(sh, v))
+        if (holds && begin_of(sh, v + 1) > begin_of(sh, v))
 #pragma unroll
           for (int g = 0; g < TG; ++g)
-            tail[g] += reinterpret_cast<const float*>(lds + at + v * p.part_stride)[g * 16 + lane];
+            tail[g] += reinterpret_cast<const float*>(lds + at + v * p.part_stride)[g * 16 + 4 * tok + j];
       store(quad, tail);
     }
   }
@@ -362,7 +359,8 @@ void launch_fmt(MatvecParams p, hipStream_t s) {
   if (p.m * x_bytes(1, p.d) > kLds - kRings)
     while (p.batches * fit < p.m) p.batches *= 2;
   p.batch = (p.m + p.batches - 1) / p.batches;
-  p.groups = p.batches == 1 ? p.shares : ((p.shares + p.batches - 1) / p.batches + 7) / 8 * 8;
+  p.each = (p.shares * p.batches + 255) / 256;
+  p.groups = p.batches == 1 ? p.shares : ((p.shares + p.each - 1) / p.each + 7) / 8 * 8;
   int64_t lds = kRings + x_bytes(p.batch, p.d);
   if (p.batches == 1) {  // one share: a wave's ring is free by the time its parts are written
     p.part_at = 0;
@@ -377,6 +375,7 @@ void launch_fmt(MatvecParams p, hipStream_t s) {
   const int tg = (p.batch + 3) / 4;
   if (tg == 1) launch_timed(matvec_kernel<FMT, 1>, grid, dim3(kThreads), (uint32_t)lds, s, p);
   else if (tg == 2) launch_timed(matvec_kernel<FMT, 2>, grid, dim3(kThreads), (uint32_t)lds, s, p);
+  else if (tg == 3) launch_timed(matvec_kernel<FMT, 3>, grid, dim3(kThreads), (uint32_t)lds, s, p);
   else launch_timed(matvec_kernel<FMT, 4>, grid, dim3(kThreads), (uint32_t)lds, s, p);
 }
 

@@ -191,4 +191,13 @@ __device__ __forceinline__ double add_swapped(double v) {
          __builtin_bit_cast(double, ((uint64_t)hi[1] << 32) | lo[1]);
 }
 
+// Two sums in one: over the lanes 32 (16) apart, of a in the lower half (even rows of 16), of b in the other.
+template <bool HALF>
+__device__ __forceinline__ float add_pair(float a, float b) {
+  u32x2 r;
+  if constexpr (HALF) r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false));
+  else r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false));
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 }  // namespace resq
