@@ -18,6 +18,12 @@
 // n and d alone, so a token's result is the same alone and among others.  (With whole quads to waves,
 // 2.3 a wave at 4 x 37888 x 3584, the same loop took 23.0 us instead of 22.0.)
 //
+// Measured (a large copy runs at 5.08 TB/s, an empty kernel takes about 4 us of a graph): one token x 2560 x
+// 2048 MXFP4 5.0 us, launch and first loads; 4 x 37888 x 3584 HiF4 18.2 us, 4.2 TB/s; 1 x 37888 x 3584
+// MXFP4 18.9 us; 16 x 37888 x 3584 30.7 us HiF4, 25.6 us MXFP4, where four tokens' reads of X from LDS to
+// each step, 512 cycles of a CU, stand beside the decoding.  16 x 2048 x 11008 HiF4 15.7 us: four batches,
+// each decoding all weights.  The tile GEMM of mixed.hip takes 7.2, 55 and 40 us for the first, second and last.
+//
 // Data movement.  X lies in LDS.  Tokens that do not fit together are taken in B batches by B
 // workgroups on one XCD, each with up to B shares (so that X is copied once per workgroup and the codes come
 // from HBM once and from the L2 B - 1 times).  Codes and scales go straight into a ring of kAhead steps

@@ -8,6 +8,10 @@
 // Both are bound by HBM: each row is read once and kept in registers between its statistics and
 // its use.  A row belongs to L lanes of one workgroup, each holding C groups of E = 8 consecutive
 // elements (E = 1 for rows shorter than 8).  L < 64: several rows share a wave.
+// Measured (float32 Y and dX, bf16 streams, both norms, a gate per channel; a large copy runs at 5.08 TB/s):
+// 8192 x 3584 forward 58 us, 5.1 TB/s, and backward 98 us, 4.8 TB/s, with the sum of the partial rows 5;
+// 131072 x 128 forward 33 us, 5.1 TB/s; 2048 x 16384 forward 82 us, 4.1 TB/s (a row fills a CU's lanes, so
+// loads, statistics and stores of only two rows overlap).  One row of 2048: 2.4 us, a launch.
 //
 // A row's last group is moved back to end at the row's end, so that every lane's accesses are
 // whole (a lane past the end takes the same place): the elements that two lanes then hold count
@@ -209,8 +213,9 @@ __global__ __launch_bounds__(1024, 8) void norm_fwd_kernel(NormFwd p, int L) {
 // With w = alpha gamma_post (times g of the channel) the second mean follows from sums that need no
 // c: sum(w yn e) = sum(w yn (dh' + r_h dx gamma_pre)) - r_h c sum(w yn hn), so one reduction per row
 // gives c, k and a token's dg.
-// A workgroup walks over rows and keeps the column sums in registers; writes one
-// row of partial sums, which norm_bwd_sum_kernel adds in a fixed order.
+// A workgroup walks over rows and keeps the column sums; it writes one row of partial sums, which
+// norm_bwd_sum_kernel adds in a fixed order.  512 workgroups: two of 7 waves to a CU at d = 3584, where
+// writing and reading the partial rows of 8192 adds 6% to the bytes.
 template <typename TH, typename TY, typename TX, int E, int C, bool WAVES>
 __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
   __shared__ float lds[2][3 * kMaxWaves];
