@@ -331,12 +331,13 @@ int resq_linear_w16a4(int format, const uint16_t* X, int64_t m, int64_t d, int64
  * resq_matvec_w4a16 - resq_linear_w4a16 for the few tokens of a rollout's tail: Y = X Q(W)^T for
  * m <= 16 rows (RESQ_ERR_UNSUPPORTED beyond), bound by one read of Q(W).
  * X: m x d bf16, any row stride ldx >= d, 2-byte aligned.  Q(W): K-major codes and scales as for
- *   resq_linear_w4a16 (codes 16-byte, HiF4 scales 4-byte aligned).  d: a multiple of the block, at
- *   most 56832 (RESQ_ERR_UNSUPPORTED beyond).
+ *   resq_linear_w4a16 (codes 16-byte, HiF4 scales 4-byte aligned).  d: a multiple of the block, below
+ *   2^30 (RESQ_ERR_UNSUPPORTED beyond).
  * Y: m x n, row stride ldy >= n, float32 (y_dtype = RESQ_IN_F32) or bf16 (RESQ_IN_BF16: the
  *   float32 result rounded once, ties to even).  d = 0 writes zeros.
- * Products are exact; the sum over d is float32, in an order fixed by n and d: a token's result is
- * the same alone and among others, and may differ from resq_linear_w4a16's in its last bits.
+ * Products are exact; the sum over d is float32, in an order fixed by m, n and d: up to m
+ * (1024 ceil(d / 512) + 16) <= 122880 by n and d alone, a token's result being the same alone and among
+ * others.  It may differ from resq_linear_w4a16's in its last bits.
  * No workspace.
  */
 int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64_t ldx,

@@ -923,7 +923,7 @@ int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64
   if (m > resq::kMatvecMaxRows)
     return fail(RESQ_ERR_UNSUPPORTED, "m (%lld) > %lld: use resq_linear_w4a16", (long long)m, (long long)resq::kMatvecMaxRows);
   if (n > INT32_MAX) return fail(RESQ_ERR_UNSUPPORTED, "n (%lld) must be below 2^31", (long long)n);
-  if (!resq::matvec_supported(d)) return fail(RESQ_ERR_UNSUPPORTED, "d (%lld) too long: use resq_linear_w4a16", (long long)d);
+  if (d >= (int64_t)1 << 30) return fail(RESQ_ERR_UNSUPPORTED, "d (%lld) must be below 2^30", (long long)d);
   if (m == 0 || n == 0) return ok();
   if (d > 0 && (!qw_codes || !qw_scales || (uintptr_t)qw_codes % 16 != 0 ||
                 (format == RESQ_HIF4 && (uintptr_t)qw_scales % 4 != 0)))

@@ -212,7 +212,6 @@ void launch_norm_bwd(NormBwd p, bool h_f32, bool y_f32, bool dx_f32, float* dgam
 // A few rows of bf16 activations (m <= kMatvecMaxRows) times 4-bit weights (matvec.hip):
 // Y[m][n] = X[m][d] Q(W)[n][d]^T, Y float32 or bf16.
 constexpr int64_t kMatvecMaxRows = 16;
-bool matvec_supported(int64_t d);  // a row of X fits the LDS beside the rings
 void launch_matvec(int fmt, const uint16_t* X, int64_t m, int64_t d, int64_t ldx, const uint8_t* codes,
                    const void* scales, int64_t n, void* Y, int64_t ldy, bool out_bf16, hipStream_t s);
 

@@ -11,25 +11,29 @@
 // block, or half a HiF4 block, with its scale.  Result register r is token r, row j, of block b's
 // elements; at the end the 16 blocks are added by lane exchange.
 //
-// Work split.  The quads of rows are dealt in contiguous ranges ("shares") to as many workgroups as
-// there are CUs, and a share's steps (a quad's 512-element steps one after the other) in equal parts to
-// the 16 waves of a workgroup: every CU and wave is busy to the end whatever the sizes.  A quad that
-// several waves have a part of is added through LDS in wave order.  The order of additions depends on
-// n and d alone, so a token's result is the same alone and among others.  (With whole quads to waves,
-// 2.3 a wave at 4 x 37888 x 3584, the same loop took 23.0 us instead of 22.0.)
+// Work split.  The quads of rows are dealt in nearly equal ranges to as many workgroups as there are CUs,
+// and a range's steps (a quad's 512-element steps one after the other) in equal parts to the 16 waves of a
+// workgroup: every CU and wave is busy to the end whatever the sizes.  A quad that several waves have a
+// part of is added through LDS in wave order.  (With whole quads to waves, 2.3 a wave at 4 x 37888 x 3584,
+// the same loop took 23.0 us instead of 22.0.)
+//
+// Data movement.  X lies in LDS.  Where not all tokens fit, either they are taken in B batches by B
+// workgroups on one XCD (the codes come from HBM once and from the L2 B - 1 times, and are decoded B times),
+// or K in windows: all weights decoded once, X copied through every CU window by window, two barriers and
+// the latency of a step a window (about 3 us).  Batches, where there are few of them and of quads.
+// Codes and scales go straight into a ring of kAhead steps in each wave's own part of LDS (buffer loads
+// with the LDS destination: a step waits for its own loads only; with loads to registers the compiler
+// waited for all in flight).  Tokens past the last repeat it and are dropped; weight rows past the last read
+// zeros.  The order of a token's additions depends on n and d alone where X fits whole, and so is its
+// result the same alone and among others.
 //
 // Measured (a large copy runs at 5.08 TB/s, an empty kernel takes about 4 us of a graph): one token x 2560 x
 // 2048 MXFP4 5.0 us, launch and first loads; 4 x 37888 x 3584 HiF4 18.2 us, 4.2 TB/s; 1 x 37888 x 3584
-// MXFP4 18.9 us; 16 x 37888 x 3584 30.7 us HiF4, 25.6 us MXFP4, where four tokens' reads of X from LDS to
-// each step, 512 cycles of a CU, stand beside the decoding.  16 x 2048 x 11008 HiF4 15.7 us: four batches,
-// each decoding all weights.  The tile GEMM of mixed.hip takes 7.2, 55 and 40 us for the first, second and last.
-//
-// Data movement.  X lies in LDS.  Tokens that do not fit together are taken in B batches by B
-// workgroups on one XCD, each with up to B shares (so that X is copied once per workgroup and the codes come
-// from HBM once and from the L2 B - 1 times).  Codes and scales go straight into a ring of kAhead steps
-// in each wave's own part of LDS (buffer loads with the LDS destination: a step waits for its own loads
-// only; with loads to registers the compiler waited for all in flight).  Tokens past the last repeat
-// it and are dropped; weight rows past the last read zeros.
+// MXFP4 18.6 us; 16 x 37888 x 3584 30 us HiF4, 26 us MXFP4, where four tokens' reads of X from LDS to
+// each step, 512 cycles of a CU, stand beside the decoding; 16 x 2048 x 11008 HiF4 14.4 us (batches);
+// 16 x 20000 x 18944 HiF4 94 us (windows; 267 in 16 batches).  The tile GEMM of mixed.hip takes 7.2 us for
+// the first, 55 for the second, 40 and 134 for the last two; it is up to a tenth faster from 13 tokens on for
+// MXFP4 rows longer than about 12000.
 //
 // Decoding.  MXFP4: a half is one 32-block, so gfx950's scaled FP4 conversion gives exact bf16
 // weights and the tile accumulates over all of K.  HiF4: an element is k/4 s1 2^-(b2+b3).  The byte
@@ -59,7 +63,16 @@ constexpr int kPad = 8;            // elements between X rows in LDS: four token
 constexpr int kSlot = 1024 + 256;  // bytes of a step's codes and scales in the ring
 constexpr int kLds = 160 * 1024;
 constexpr int kRings = kWaves * kAhead * kSlot;
-constexpr int kParts = kWaves * 16 * 16;  // bytes of the waves' parts of quads, 16 tokens x 4 rows each
+constexpr int kQuadBytes = 16 * 16;            // a quad's sums, 16 tokens x 4 rows
+constexpr int kParts = kWaves * kQuadBytes;    // the waves' parts of quads
+constexpr int kBlockQuads = 48;                // quads whose sums wait in LDS where X does not fit whole
+constexpr int kPieces = 6;                     // 16-byte pieces of X of a thread meanwhile
+// Batches of tokens, each with X whole in LDS, instead of windows of K: at most so many, and so many quads
+// times batches.  (HiF4: 16 x 2048 x 11008, 4 batches of 512 quads: 14.4 us in batches, 21.5 in windows.  16 x
+// 9215 x 12864, 4 of 2304: 50 and 43.  16 x 3412 x 17408, 6 of 853: 60 and 36.)
+constexpr int kMaxBatches = 4, kMaxBatchQuads = 2048;
+// Steps of K in LDS at a time, a window: for TG groups of four tokens.
+constexpr int window_of(int tg) { return kPieces * kWaves / (4 * tg); }
 
 struct MatvecParams {
   const uint16_t* X;
@@ -69,10 +82,9 @@ struct MatvecParams {
   void* Y;
   int64_t ldy, n;
   int m, d;
-  int batch, batches;     // tokens in LDS at a time
-  int shares, each, groups;  // shares of quads, of a workgroup; workgroups per batch, a multiple of 8 (one XCD per share)
-  int quads, quads_left;  // quads per share; the first quads_left shares have one more
-  int part_at, part_stride, part_flip;  // LDS of a wave's parts of quads; distance of two shares' (B > 1)
+  int quads, quads_left;  // quads per workgroup; the first quads_left have one more
+  int batch, groups;      // tokens of a workgroup, and workgroups per batch, where X lies whole in LDS
+  int windows, window;    // of K, and their steps, where X does not fit whole
   bool out_bf16;
 };
 
@@ -119,83 +131,179 @@ __device__ __forceinline__ void hif4_bf16(uint32_t w, float s0, float s1, uint32
   out[3] = fp8_pair<1>(hi, s1);
 }
 
-// TG: groups of four tokens in a batch.
-template <int FMT, int TG>
-__global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // rings, X, parts
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j = lane & 3, blk = lane >> 2;
-  const int turns = (p.d + kStep - 1) / kStep;
-  const int t0 = (int)(blockIdx.x / p.groups) * p.batch, tokens = min(p.batch, p.m - t0);  // may be none
-  const int share0 = (int)(blockIdx.x % p.groups) * p.each, share1 = min(p.shares, share0 + p.each);
-  if (share0 >= share1 || tokens <= 0) return;
-
-  // A share's steps, and those of a wave (parts that differ by one at most).
-  auto quads_of = [&](int sh) { return p.quads + (sh < p.quads_left ? 1 : 0); };
-  auto begin_of = [&](int sh, int v) {
-    const uint32_t all = (uint32_t)quads_of(sh) * turns;
-    return v * (all / kWaves) + min((uint32_t)v, all % kWaves);
-  };
-  auto first_quad = [&](int sh) { return sh * p.quads + min(sh, p.quads_left); };
-
-  uint8_t* ring = lds + wave * (kAhead * kSlot);
-  uint16_t* xs = reinterpret_cast<uint16_t*>(lds + kRings);
-  const int width = turns * kStep, stride = width + kPad;  // a row of X, zeros past d
-  const int per_row = width / 8, t_step = kThreads / per_row, c_step = kThreads % per_row;
-
-  // Loads of the wave's steps, one after the other through its shares, into slot after slot.
-  const int64_t code_row = p.d / 2, scale_row = FMT == 0 ? p.d / 32 : p.d / 64 * 4;
-  const uint32_t mis = (uint32_t)(uintptr_t)p.scales & 3u;  // MXFP4: scales go as the aligned dwords around them
-  const uint32_t code_at = (uint32_t)(j * code_row) + 16 * blk;
-  const uint32_t scale_at = (uint32_t)(j * scale_row) + (FMT == 0 ? mis + blk : 4 * (blk >> 1));
+// The loads of a wave's steps: codes and scales of a quad's 512-element steps into slot after slot of its ring.
+template <int FMT>
+struct Weights {
+  const MatvecParams& p;
+  uint8_t* ring;
+  int64_t code_row, scale_row;
+  uint32_t mis;  // MXFP4: scales go as the aligned dwords around them
+  uint32_t code_at, scale_at;
   __amdgpu_buffer_rsrc_t code_buf, scale_buf;
-  int load_share = share0 - 1, load_left = 0, load_quad = 0, load_turn = 0, load_slot = 0;
-  auto seek = [&]() {  // a quad's four rows, as far as the matrix has them
-    const int64_t row = 4 * (int64_t)load_quad, rows = min((int64_t)4, p.n - row);
+  int load_slot = 0, slot = 0;
+  int in_flight = 0;
+
+  __device__ Weights(const MatvecParams& p_, uint8_t* ring_, int lane) : p(p_), ring(ring_) {
+    const int j = lane & 3, blk = lane >> 2;
+    code_row = p.d / 2;
+    scale_row = FMT == 0 ? p.d / 32 : p.d / 64 * 4;
+    mis = (uint32_t)(uintptr_t)p.scales & 3u;
+    code_at = (uint32_t)(j * code_row) + 16 * blk;
+    scale_at = (uint32_t)(j * scale_row) + (FMT == 0 ? mis + blk : 4 * (blk >> 1));
+  }
+  __device__ void seek(int64_t quad) {  // a quad's four rows, as far as the matrix has them
+    const int64_t row = 4 * quad, rows = min((int64_t)4, p.n - row);
     code_buf = buffer(p.codes + row * code_row, rows * code_row);
     scale_buf = buffer(p.scales + row * scale_row - mis, (rows * scale_row + mis + 3) & ~3ll);
-  };
-  auto more = [&]() {  // moves to the next share with steps left; false: none
-    while (load_left == 0) {
-      if (++load_share >= share1) return false;
-      const uint32_t b = begin_of(load_share, wave);
-      load_left = (int)(begin_of(load_share, wave + 1) - b);
-      if (load_left == 0) continue;
-      load_quad = first_quad(load_share) + (int)(b / (uint32_t)turns);
-      load_turn = (int)(b % (uint32_t)turns);
-      seek();
-    }
-    return true;
-  };
-  auto load = [&]() {
-    const uint32_t k = load_turn * kStep;
+  }
+  __device__ void load(int turn) {
+    const uint32_t k = turn * kStep;
     uint8_t* dst = ring + load_slot * kSlot;
     copy16(code_buf, dst, code_at + k / 2);
     const uint32_t at = scale_at + (FMT == 0 ? k / 32 : k / 16);
     copy4(scale_buf, dst + 1024, FMT == 0 ? at & ~3u : at);
     load_slot = load_slot + 1 == kAhead ? 0 : load_slot + 1;
-    if (--load_left > 0 && ++load_turn == turns) {
-      load_turn = 0;
-      ++load_quad;
-      seek();
-    }
-  };
-  int in_flight = 0;
-  while (in_flight < kAhead && more()) {
-    load();
     ++in_flight;
   }
+  // The oldest step's codes and scale, once they have landed; its slot is free.
+  __device__ void take(int lane, int turn, int turns, u32x4& w, uint32_t& sc) {
+    const uint8_t* src = ring + slot * kSlot;
+    w = *reinterpret_cast<const u32x4*>(src + 16 * lane);
+    sc = *reinterpret_cast<const uint32_t*>(src + 1024 + 4 * lane);
+    if constexpr (FMT == 0) {
+      sc = (sc >> (8 * (scale_at & 3u))) & 0xFFu;
+      // past the row's end the code may be any row's: a finite one, against zeros of X
+      if (turn == turns - 1 && turn * kStep + 32 * (lane >> 2) >= p.d) sc = 127u;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+    --in_flight;
+    slot = slot + 1 == kAhead ? 0 : slot + 1;
+  }
+};
 
-  // X of the batch into LDS, in pieces of eight elements: piece tid, tid + kThreads, ..
+// Eight elements of X in the order hif4_bf16 gives.
+template <int FMT>
+__device__ __forceinline__ u32x4 in_order(const u32x4& o) {
+  if constexpr (FMT == 0) return o;
+  return u32x4{__builtin_amdgcn_perm(o[1], o[0], 0x05040100u), __builtin_amdgcn_perm(o[1], o[0], 0x07060302u),
+               __builtin_amdgcn_perm(o[3], o[2], 0x05040100u), __builtin_amdgcn_perm(o[3], o[2], 0x07060302u)};
+}
+
+// A step's products: sum[g] gets tokens 4 g .. 4 g + 3 by the quad's rows.
+template <int FMT, int TG>
+__device__ __forceinline__ void multiply(f32x4 sum[TG], const uint16_t* const xlane[TG], int at, const u32x4& w, uint32_t sc,
+                                         int blk) {
+  uint32_t v[4][4];
+  if constexpr (FMT == 0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mx_dequant8(w[q], sc, v[q]);
+  } else {
+    const uint32_t h = blk & 1, b2 = sc >> (8 + 4 * h), b3 = sc >> (16 + 8 * h);
+    const uint32_t lo = hif4_steps(b2, b3), hi = hif4_steps(b2 >> 2, b3 >> 4);
+    hif4_bf16(w[0], (float)(lo & 0xFFu), (float)((lo >> 8) & 0xFFu), v[0]);
+    hif4_bf16(w[1], (float)((lo >> 16) & 0xFFu), (float)(lo >> 24), v[1]);
+    hif4_bf16(w[2], (float)(hi & 0xFFu), (float)((hi >> 8) & 0xFFu), v[2]);
+    hif4_bf16(w[3], (float)((hi >> 16) & 0xFFu), (float)(hi >> 24), v[3]);
+  }
+#pragma unroll
+  for (int g = 0; g < TG; ++g) {
+    f32x4 r = FMT == 0 ? sum[g] : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(xlane[g] + at + 8 * q);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x2 a = {x[2 * e], x[2 * e + 1]}, b = {v[q][2 * e], v[q][2 * e + 1]};
+        r = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), r, 0, 0, 0);
+      }
+    }
+    if constexpr (FMT == 0) {
+      sum[g] = r;
+    } else {
+      // s1 = 2^(e-31) (1 + m/4) for code 4 e + m
+      const float s1 = __uint_as_float(((sc & 0xFFu) << 21) + ((127u - 31u) << 23));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[g][i] = fmaf(s1, r[i], sum[g][i]);
+    }
+  }
+}
+
+// The 16 blocks' sums added, the four tokens' in one go: lane 16 r + j (j < 4) gets token r of row j.
+// Clears them.
+template <int TG>
+__device__ __forceinline__ void reduce(f32x4 sum[TG], float out[TG]) {
+#pragma unroll
+  for (int g = 0; g < TG; ++g) {
+    float v = add_pair<false>(add_pair<true>(sum[g][0], sum[g][2]), add_pair<true>(sum[g][1], sum[g][3]));
+    v += dpp<kDppRor8>(v);
+    out[g] = v + dpp<kDppRor4>(v);
+    sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+// The lanes whose sum of reduce is the one that is kept: of token 4 g + (lane >> 4), row lane & 3.
+__device__ __forceinline__ bool holds(int lane) { return (lane & 12) == 0; }
+// Their place in a quad's sums in LDS, 16 floats to a group of tokens.
+__device__ __forceinline__ int quad_at(int lane) { return 4 * (lane >> 4) + (lane & 3); }
+
+template <int TG>
+__device__ __forceinline__ void store(const MatvecParams& p, int64_t quad, const float v[TG], int lane) {
+  const int64_t row = 4 * quad + (lane & 3);
+  if (!holds(lane) || row >= p.n) return;
+#pragma unroll
+  for (int g = 0; g < TG; ++g) {
+    const int t = 4 * g + (lane >> 4);
+    if (t >= p.m) continue;
+    const int64_t at = (int64_t)t * p.ldy + row;
+    if (p.out_bf16) reinterpret_cast<uint16_t*>(p.Y)[at] = bf16_bits(v[g]);
+    else reinterpret_cast<float*>(p.Y)[at] = v[g];
+  }
+}
+
+// Part v of n steps dealt to the waves: the first.
+__device__ __forceinline__ uint32_t begin_of(uint32_t n, int v) { return v * (n / kWaves) + min((uint32_t)v, n % kWaves); }
+
+// X of a batch of tokens whole in LDS.  TG: groups of four tokens.
+template <int FMT, int TG>
+__global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // rings (the waves' parts at the end), X
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = lane & 3, blk = lane >> 2;
+  const int turns = (p.d + kStep - 1) / kStep, wg = blockIdx.x % p.groups, t0 = (int)(blockIdx.x / p.groups) * p.batch;
+  const uint32_t all = (uint32_t)(p.quads + (wg < p.quads_left ? 1 : 0)) * turns;
+  if (all == 0 || t0 >= p.m) return;
+  p.X += t0 * p.ldx;
+  p.Y = reinterpret_cast<uint8_t*>(p.Y) + t0 * p.ldy * (p.out_bf16 ? 2 : 4);
+  p.m = min(p.batch, p.m - t0);
+  const int64_t q0 = (int64_t)wg * p.quads + min(wg, p.quads_left);
+  const uint32_t begin = begin_of(all, wave);
+  const int count = (int)(begin_of(all, wave + 1) - begin);
+
+  Weights<FMT> weights(p, lds + wave * (kAhead * kSlot), lane);
+  int64_t load_quad = q0 + begin / (uint32_t)turns;
+  int load_turn = (int)(begin % (uint32_t)turns), load_left = count;
+  if (load_left > 0) weights.seek(load_quad);
+  auto load = [&]() {
+    weights.load(load_turn);
+    if (--load_left > 0 && ++load_turn == turns) {
+      load_turn = 0;
+      weights.seek(++load_quad);
+    }
+  };
+  for (int i = 0; i < kAhead && load_left > 0; ++i) load();
+
+  // X in pieces of eight elements: piece tid, tid + kThreads, ..
+  uint16_t* xs = reinterpret_cast<uint16_t*>(lds + kRings);
+  const int width = turns * kStep, stride = width + kPad;  // a row of X, zeros past d
+  const int per_row = width / 8, t_step = kThreads / per_row, c_step = kThreads % per_row;
   int t = tid / per_row, c = tid - t * per_row;
-  while (t < tokens) {
+  while (t < p.m) {
     u32x4 v[8];
     uint16_t* dst[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       v[i] = u32x4{0u, 0u, 0u, 0u};
-      dst[i] = t < tokens ? xs + t * stride + 8 * c : nullptr;
-      if (t < tokens && 8 * c < p.d) v[i] = reinterpret_cast<const Bf16x8*>(p.X + (int64_t)(t0 + t) * p.ldx + 8 * c)->v;
+      dst[i] = t < p.m ? xs + t * stride + 8 * c : nullptr;
+      if (t < p.m && 8 * c < p.d) v[i] = reinterpret_cast<const Bf16x8*>(p.X + (int64_t)t * p.ldx + 8 * c)->v;
       t += t_step;
       c += c_step;
       if (c >= per_row) {
@@ -205,11 +313,7 @@ __global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      u32x4 o = v[i];
-      if constexpr (FMT != 0)  // in the order hif4_bf16 gives: 0 2 1 3 4 6 5 7
-        o = u32x4{__builtin_amdgcn_perm(o[1], o[0], 0x05040100u), __builtin_amdgcn_perm(o[1], o[0], 0x07060302u),
-                  __builtin_amdgcn_perm(o[3], o[2], 0x05040100u), __builtin_amdgcn_perm(o[3], o[2], 0x07060302u)};
-      if (dst[i]) *reinterpret_cast<u32x4*>(dst[i]) = o;
+      if (dst[i]) *reinterpret_cast<u32x4*>(dst[i]) = in_order<FMT>(v[i]);
     }
   }
   lds_barrier();
@@ -217,128 +321,239 @@ __global__ __launch_bounds__(kThreads) void matvec_kernel(MatvecParams p) {
   f32x4 sum[TG] = {};
   const uint16_t* xlane[TG];
 #pragma unroll
-  for (int g = 0; g < TG; ++g) xlane[g] = xs + min(4 * g + j, tokens - 1) * stride + 32 * blk;
-  auto multiply = [&](int at, const u32x4& w, uint32_t sc) {
-    uint32_t v[4][4];
-    if constexpr (FMT == 0) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) mx_dequant8(w[q], sc, v[q]);
-    } else {
-      const uint32_t h = blk & 1, b2 = sc >> (8 + 4 * h), b3 = sc >> (16 + 8 * h);
-      const uint32_t lo = hif4_steps(b2, b3), hi = hif4_steps(b2 >> 2, b3 >> 4);
-      hif4_bf16(w[0], (float)(lo & 0xFFu), (float)((lo >> 8) & 0xFFu), v[0]);
-      hif4_bf16(w[1], (float)((lo >> 16) & 0xFFu), (float)(lo >> 24), v[1]);
-      hif4_bf16(w[2], (float)(hi & 0xFFu), (float)((hi >> 8) & 0xFFu), v[2]);
-      hif4_bf16(w[3], (float)((hi >> 16) & 0xFFu), (float)(hi >> 24), v[3]);
-    }
-#pragma unroll
-    for (int g = 0; g < TG; ++g) {
-      f32x4 r = FMT == 0 ? sum[g] : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(xlane[g] + at + 8 * q);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const u32x2 a = {x[2 * e], x[2 * e + 1]}, b = {v[q][2 * e], v[q][2 * e + 1]};
-          r = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), r, 0, 0, 0);
-        }
-      }
-      if constexpr (FMT == 0) {
-        sum[g] = r;
+  for (int g = 0; g < TG; ++g) xlane[g] = xs + min(4 * g + j, p.m - 1) * stride + 32 * blk;
+  int64_t quad = q0 + begin / (uint32_t)turns;
+  int turn = (int)(begin % (uint32_t)turns);
+  bool whole = turn == 0;  // this wave has the quad from its first step on
+  float head[TG] = {};     // of a quad that an earlier wave began
+  for (int s = 0; s < count; ++s) {
+    if (weights.in_flight == kAhead) wait_vm<2 * (kAhead - 1)>();
+    else wait_vm<0>();
+    u32x4 w;
+    uint32_t sc;
+    weights.take(lane, turn, turns, w, sc);
+    if (load_left > 0) load();
+    multiply<FMT, TG>(sum, xlane, turn * kStep, w, sc, blk);
+    if (++turn == turns) {
+      float v[TG];
+      reduce<TG>(sum, v);
+      if (whole) {
+        store<TG>(p, quad, v, lane);
       } else {
-        // s1 = 2^(e-31) (1 + m/4) for code 4 e + m
-        const float s1 = __uint_as_float(((sc & 0xFFu) << 21) + ((127u - 31u) << 23));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[g][i] = fmaf(s1, r[i], sum[g][i]);
+        for (int g = 0; g < TG; ++g) head[g] = v[g];
       }
+      whole = true;
+      turn = 0;
+      ++quad;
+    }
+  }
+  // Shared quads: each wave leaves its part of a quad that an earlier wave began, in its ring.
+  float tail[TG];
+  reduce<TG>(sum, tail);
+  const bool inside = count > 0 && !whole;  // its only quad neither begins nor ends here
+  if (holds(lane))
+#pragma unroll
+    for (int g = 0; g < TG; ++g)
+      reinterpret_cast<float*>(lds + wave * (kAhead * kSlot))[g * 16 + quad_at(lane)] = inside ? tail[g] : head[g];
+  lds_barrier();
+  if (whole && turn > 0) {  // this wave began the quad: add the waves after it up to the quad's end
+    const uint32_t end = (uint32_t)(quad - q0 + 1) * turns;
+    for (int v = wave + 1; v < kWaves && begin_of(all, v) < end; ++v)
+      if (holds(lane) && begin_of(all, v + 1) > begin_of(all, v))
+#pragma unroll
+        for (int g = 0; g < TG; ++g)
+          tail[g] += reinterpret_cast<const float*>(lds + v * (kAhead * kSlot))[g * 16 + quad_at(lane)];
+    store<TG>(p, quad, tail, lane);
+  }
+}
+
+// X in windows of K: while one in LDS is used the next is on its way to registers.  A block of quads goes
+// through all windows; a window's steps, quad by quad, are dealt to the waves like all steps above, in the
+// same way in every window, so that a quad's sum in LDS belongs to one wave.
+template <int FMT, int TG>
+__global__ __launch_bounds__(kThreads) void matvec_windows_kernel(MatvecParams p) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // rings, parts, sums, X
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = lane & 3, blk = lane >> 2;
+  const int turns = (p.d + kStep - 1) / kStep, wg = blockIdx.x;
+  const int quads = p.quads + (wg < p.quads_left ? 1 : 0);
+  const int64_t q0 = (int64_t)wg * p.quads + min(wg, p.quads_left);
+  float* parts = reinterpret_cast<float*>(lds + kRings);
+  float* sums = reinterpret_cast<float*>(lds + kRings + kParts);
+  uint16_t* xs = reinterpret_cast<uint16_t*>(lds + kRings + kParts + kBlockQuads * kQuadBytes);
+  const int stride = p.window * kStep + kPad;
+  const int blocks = (quads + kBlockQuads - 1) / kBlockQuads;
+  const int64_t rounds = (int64_t)blocks * p.windows;  // (block, window) pairs, one after the other
+  auto quads_of = [&](int block) { return min(kBlockQuads, quads - block * kBlockQuads); };
+  auto turns_of = [&](int window) { return min(p.window, turns - window * p.window); };
+
+  // The steps of the wave, as a cursor for the loads and one for the products.
+  struct Cursor {
+    int block, window;     // blocks: past the end
+    uint32_t at, end;      // of the round's steps
+    int quad, turn;
+    uint32_t begin;        // of every round of the block: the first step, its quad and turn
+    int quad0, turn0;
+  };
+  auto enter = [&](Cursor& u) {  // a block's steps of this wave
+    const uint32_t all = (uint32_t)quads_of(u.block) * p.window;
+    u.at = u.begin = begin_of(all, wave);
+    u.end = begin_of(all, wave + 1);
+    u.quad = u.quad0 = (int)(u.at / (uint32_t)p.window);
+    u.turn = u.turn0 = (int)(u.at % (uint32_t)p.window);
+  };
+  auto next_round = [&](Cursor& u) {
+    if (++u.window == p.windows) {
+      u.window = 0;
+      if (++u.block < blocks) enter(u);
+    } else {
+      u.at = u.begin;
+      u.quad = u.quad0;
+      u.turn = u.turn0;
     }
   };
-  // The 16 blocks' sums added, the four tokens' in one go: lane 16 r + j (j < 4) gets token r of row j.
-  // Clears them.
-  auto reduce = [&](float out[TG]) {
-#pragma unroll
-    for (int g = 0; g < TG; ++g) {
-      float v = add_pair<false>(add_pair<true>(sum[g][0], sum[g][2]), add_pair<true>(sum[g][1], sum[g][3]));
-      v += dpp<kDppRor8>(v);
-      out[g] = v + dpp<kDppRor4>(v);
-      sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  };
-  const bool holds = (blk & 3) == 0;  // this lane's sum is the one that is kept: of token 4 g + tok
-  const int tok = lane >> 4;
-  auto store = [&](int quad, const float v[TG]) {
-    const int64_t row = 4 * (int64_t)quad + j;
-    if (!holds || row >= p.n) return;
-#pragma unroll
-    for (int g = 0; g < TG; ++g) {
-      const int tk = 4 * g + tok;
-      if (tk >= tokens) continue;
-      const int64_t at = (int64_t)(t0 + tk) * p.ldy + row;
-      if (p.out_bf16) reinterpret_cast<uint16_t*>(p.Y)[at] = bf16_bits(v[g]);
-      else reinterpret_cast<float*>(p.Y)[at] = v[g];
+  auto advance = [&](Cursor& u) {
+    ++u.at;
+    if (++u.turn == p.window) {
+      u.turn = 0;
+      ++u.quad;
     }
   };
 
-  int slot = 0;
-  for (int sh = share0; sh < share1; ++sh) {
-    const uint32_t begin = begin_of(sh, wave);
-    const int q0 = first_quad(sh), count = (int)(begin_of(sh, wave + 1) - begin);
-    int quad = q0 + (int)(begin / (uint32_t)turns), turn = (int)(begin % (uint32_t)turns);
-    bool whole = turn == 0;  // this wave has the quad from its first step on
-    float head[TG] = {};     // of a quad that an earlier wave began
-    for (int s = 0; s < count; ++s) {
-      if (in_flight == kAhead) wait_vm<2 * (kAhead - 1)>();
-      else wait_vm<0>();
-      const uint8_t* src = ring + slot * kSlot;
-      const u32x4 w = *reinterpret_cast<const u32x4*>(src + 16 * lane);
-      uint32_t sc = *reinterpret_cast<const uint32_t*>(src + 1024 + 4 * lane);
-      if constexpr (FMT == 0) {
-        sc = (sc >> (8 * (scale_at & 3u))) & 0xFFu;
-        // past the row's end the code may be any row's: a finite one, against zeros of X
-        if (turn == turns - 1 && turn * kStep + 32 * blk >= p.d) sc = 127u;
+  Weights<FMT> weights(p, lds + wave * (kAhead * kSlot), lane);
+  Cursor ld{};
+  enter(ld);
+  int64_t sought = -1;
+  auto load_next = [&]() {  // the next step that K has, if any
+    while (ld.block < blocks) {
+      if (ld.at >= ld.end) {
+        next_round(ld);
+        continue;
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
-      --in_flight;
-      if (more()) {
-        load();
-        ++in_flight;
+      if (ld.turn < turns_of(ld.window)) {
+        const int64_t quad = q0 + ld.block * kBlockQuads + ld.quad;
+        if (quad != sought) weights.seek(sought = quad);
+        weights.load(ld.window * p.window + ld.turn);
+        advance(ld);
+        return true;
       }
-      multiply(turn * kStep, w, sc);
-      slot = slot + 1 == kAhead ? 0 : slot + 1;
-      if (++turn == turns) {
+      advance(ld);
+    }
+    return false;
+  };
+
+  // A window of X: pieces tid, tid + kThreads, .. of eight elements (a wave's 64 lie in one step of one token).
+  // Every thread loads kPieces, whether it keeps them or not: the waits count them.
+  u32x4 piece[kPieces];
+  int token[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) token[i] = (i * kWaves + wave) / p.window;
+  auto load_x = [&](int window) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int t = token[i], c = i * kWaves + wave - t * p.window;
+      const int k = (window * p.window + c) * kStep + 8 * lane;
+      piece[i] = reinterpret_cast<const Bf16x8*>(p.X + (int64_t)min(t, p.m - 1) * p.ldx + min(k, p.d - 8))->v;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+  };
+  auto keep_x = [&](int window) {  // zeros past d
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int t = token[i], c = i * kWaves + wave - t * p.window;
+      const int k = (window * p.window + c) * kStep + 8 * lane;
+      if (t < p.m)
+        *reinterpret_cast<u32x4*>(xs + t * stride + c * kStep + 8 * lane) = k < p.d ? in_order<FMT>(piece[i]) : u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  load_x(0);
+  for (int i = 0; i < kAhead; ++i)
+    if (!load_next()) break;
+  keep_x(0);
+  lds_barrier();
+
+  const uint16_t* xlane[TG];
+#pragma unroll
+  for (int g = 0; g < TG; ++g) xlane[g] = xs + min(4 * g + j, p.m - 1) * stride + 32 * blk;
+  f32x4 sum[TG] = {};
+  Cursor at{};
+  enter(at);
+  for (int64_t round = 0; round < rounds; ++round) {
+    const int have = turns_of(at.window);
+    const bool first = at.window == 0, last = at.window == p.windows - 1, more = round + 1 < rounds;
+    const int64_t block_quad = q0 + at.block * kBlockQuads;
+    int before = 0;  // steps in flight that were loaded before X
+    if (more) {
+      before = weights.in_flight;
+      load_x(last ? 0 : at.window + 1);
+    }
+    // A quad's sum over this and the earlier windows; after the last it is stored.
+    auto add = [&](int quad, float v[TG]) {
+      float* q = sums + quad * (kQuadBytes / 4) + quad_at(lane);
+      if (!first && holds(lane))
+#pragma unroll
+        for (int g = 0; g < TG; ++g) v[g] += q[16 * g];
+      if (last) store<TG>(p, block_quad + quad, v, lane);
+      else if (holds(lane))
+#pragma unroll
+        for (int g = 0; g < TG; ++g) q[16 * g] = v[g];
+    };
+    const bool any = at.end > at.at;
+    bool whole = at.turn == 0;  // this wave has the quad from its first step on
+    float head[TG] = {};        // of a quad that an earlier wave began
+    while (at.at < at.end) {
+      if (at.turn < have) {
+        const bool younger = weights.in_flight > 1;  // a step loaded after this one; X too if this one was before
+        if (before > 0) {
+          if (younger) wait_vm<2 + kPieces>();
+          else wait_vm<kPieces>();
+          --before;
+        } else {
+          if (younger) wait_vm<2>();
+          else wait_vm<0>();
+        }
+        const int turn = at.window * p.window + at.turn;
+        u32x4 w;
+        uint32_t sc;
+        weights.take(lane, turn, turns, w, sc);
+        load_next();
+        multiply<FMT, TG>(sum, xlane, at.turn * kStep, w, sc, blk);
+      }
+      const int quad = at.quad;
+      advance(at);
+      if (at.turn == 0) {
         float v[TG];
-        reduce(v);
+        reduce<TG>(sum, v);
         if (whole) {
-          store(quad, v);
+          add(quad, v);
         } else {
 #pragma unroll
           for (int g = 0; g < TG; ++g) head[g] = v[g];
         }
         whole = true;
-        turn = 0;
-        ++quad;
       }
     }
-    // Shared quads: each wave leaves its part of a quad that an earlier wave began.  (Two shares' parts
-    // lie apart: a wave may be in the next share's steps while another still adds.)
+    // Shared quads, as above.
     float tail[TG];
-    reduce(tail);
-    const bool inside = count > 0 && !whole;  // its only quad neither begins nor ends here
-    const int at = p.part_at + ((sh - share0) & 1) * p.part_flip;
-    if (holds)
+    reduce<TG>(sum, tail);
+    const bool inside = any && !whole;
+    if (holds(lane))
 #pragma unroll
-      for (int g = 0; g < TG; ++g)
-        reinterpret_cast<float*>(lds + at + wave * p.part_stride)[g * 16 + 4 * tok + j] = inside ? tail[g] : head[g];
-    lds_barrier();
-    if (whole && turn > 0) {  // this wave began the quad: add the waves after it up to the quad's end
-      const uint32_t end = (uint32_t)(quad - q0 + 1) * turns;
-      for (int v = wave + 1; v < kWaves && begin_of(sh, v) < end; ++v)
-        if (holds && begin_of(sh, v + 1) > begin_of(sh, v))
+      for (int g = 0; g < TG; ++g) parts[wave * (kQuadBytes / 4) + g * 16 + quad_at(lane)] = inside ? tail[g] : head[g];
+    lds_barrier();  // the window has been read, the parts are there
+    if (more) keep_x(last ? 0 : at.window + 1);
+    if (any && whole && at.turn > 0) {
+      const uint32_t all = (uint32_t)quads_of(at.block) * p.window, end = (uint32_t)(at.quad + 1) * p.window;
+      for (int v = wave + 1; v < kWaves && begin_of(all, v) < end; ++v)
+        if (holds(lane) && begin_of(all, v + 1) > begin_of(all, v))
 #pragma unroll
-          for (int g = 0; g < TG; ++g)
-            tail[g] += reinterpret_cast<const float*>(lds + at + v * p.part_stride)[g * 16 + 4 * tok + j];
-      store(quad, tail);
+          for (int g = 0; g < TG; ++g) tail[g] += parts[v * (kQuadBytes / 4) + g * 16 + quad_at(lane)];
+      add(at.quad, tail);
     }
+    lds_barrier();
+    next_round(at);
   }
 }
 
@@ -352,42 +567,53 @@ __global__ __launch_bounds__(256) void matvec_zero_kernel(MatvecParams p) {
   }
 }
 
-int64_t x_bytes(int64_t tokens, int64_t d) { return tokens * ((d + kStep - 1) / kStep * kStep + kPad) * 2; }
+int64_t x_bytes(int64_t tokens, int64_t turns) { return tokens * (turns * kStep + kPad) * 2; }
+
+// Workgroups of a batch or of all: the quads in nearly equal ranges.
+void deal(MatvecParams& p, int64_t wgs) {
+  const int64_t quads = (p.n + 3) / 4;
+  p.groups = (int)wgs;
+  p.quads = (int)(quads / wgs);
+  p.quads_left = (int)(quads % wgs);
+}
+template <int FMT>
+void launch_whole(const MatvecParams& p, int batches, uint32_t lds, hipStream_t s) {
+  const dim3 grid((unsigned)(p.groups * batches)), block(kThreads);
+  const int tg = (p.batch + 3) / 4;
+  if (tg == 1) launch_timed(matvec_kernel<FMT, 1>, grid, block, lds, s, p);
+  else if (tg == 2) launch_timed(matvec_kernel<FMT, 2>, grid, block, lds, s, p);
+  else if (tg == 3) launch_timed(matvec_kernel<FMT, 3>, grid, block, lds, s, p);
+  else launch_timed(matvec_kernel<FMT, 4>, grid, block, lds, s, p);
+}
+template <int FMT, int TG>
+void launch_windows(MatvecParams p, int64_t turns, hipStream_t s) {
+  p.windows = (int)((turns + window_of(TG) - 1) / window_of(TG));
+  p.window = (int)((turns + p.windows - 1) / p.windows);
+  constexpr int kFixed = kRings + kParts + kBlockQuads * kQuadBytes;
+  static_assert(kFixed + 4 * TG * (window_of(TG) * kStep + kPad) * 2 <= kLds, "LDS");
+  const uint32_t lds = (uint32_t)(kFixed + x_bytes(p.m, p.window));
+  launch_timed(matvec_windows_kernel<FMT, TG>, dim3((unsigned)p.groups), dim3(kThreads), lds, s, p);
+}
 
 template <int FMT>
 void launch_fmt(MatvecParams p, hipStream_t s) {
-  const int64_t quads = (p.n + 3) / 4;
-  p.shares = (int)std::min<int64_t>(quads, 256);
-  p.quads = (int)(quads / p.shares);
-  p.quads_left = (int)(quads % p.shares);
-  const int fit = (int)((kLds - kRings - 2 * kParts) / x_bytes(1, p.d));
-  p.batches = 1;  // a power of two: with 256 shares every CU gets one workgroup
-  if (p.m * x_bytes(1, p.d) > kLds - kRings)
-    while (p.batches * fit < p.m) p.batches *= 2;
-  p.batch = (p.m + p.batches - 1) / p.batches;
-  p.each = (p.shares * p.batches + 255) / 256;
-  p.groups = p.batches == 1 ? p.shares : ((p.shares + p.each - 1) / p.each + 7) / 8 * 8;
-  int64_t lds = kRings + x_bytes(p.batch, p.d);
-  if (p.batches == 1) {  // one share: a wave's ring is free by the time its parts are written
-    p.part_at = 0;
-    p.part_stride = kAhead * kSlot;
-  } else {
-    p.part_at = (int)lds;
-    p.part_stride = kParts / kWaves;
-    p.part_flip = kParts;
-    lds += 2 * kParts;
+  const int64_t quads = (p.n + 3) / 4, turns = (p.d + kStep - 1) / kStep, fit = (kLds - kRings) / x_bytes(1, turns);
+  const int64_t batches = fit > 0 ? (p.m + fit - 1) / fit : p.m;
+  if (batches == 1 || (fit > 0 && batches <= kMaxBatches && quads * batches <= kMaxBatchQuads)) {
+    p.batch = (int)((p.m + batches - 1) / batches);
+    deal(p, batches == 1 ? std::min<int64_t>(quads, 256) : std::min<int64_t>((quads + 7) / 8 * 8, 256 / batches / 8 * 8));
+    launch_whole<FMT>(p, (int)batches, (uint32_t)(kRings + x_bytes(p.batch, turns)), s);
+    return;
   }
-  const dim3 grid((unsigned)(p.groups * p.batches));
-  const int tg = (p.batch + 3) / 4;
-  if (tg == 1) launch_timed(matvec_kernel<FMT, 1>, grid, dim3(kThreads), (uint32_t)lds, s, p);
-  else if (tg == 2) launch_timed(matvec_kernel<FMT, 2>, grid, dim3(kThreads), (uint32_t)lds, s, p);
-  else if (tg == 3) launch_timed(matvec_kernel<FMT, 3>, grid, dim3(kThreads), (uint32_t)lds, s, p);
-  else launch_timed(matvec_kernel<FMT, 4>, grid, dim3(kThreads), (uint32_t)lds, s, p);
+  deal(p, std::min<int64_t>(quads, 256));
+  const int tg = (p.m + 3) / 4;
+  if (tg == 1) launch_windows<FMT, 1>(p, turns, s);
+  else if (tg == 2) launch_windows<FMT, 2>(p, turns, s);
+  else if (tg == 3) launch_windows<FMT, 3>(p, turns, s);
+  else launch_windows<FMT, 4>(p, turns, s);
 }
 
 }  // namespace
-
-bool matvec_supported(int64_t d) { return kRings + 2 * kParts + x_bytes(1, d) <= kLds; }
 
 void launch_matvec(int fmt, const uint16_t* X, int64_t m, int64_t d, int64_t ldx, const uint8_t* codes,
                    const void* scales, int64_t n, void* Y, int64_t ldy, bool out_bf16, hipStream_t s) {

@@ -44,10 +44,16 @@ def test_more_rows_than_a_grid_dimension_holds():
     assert torch.equal(got[2], want[2].repeat(1, times)[:, :m])
 
 
+def _whole(m, d):
+    """X lies whole in LDS: the order of a sum depends on n and d alone."""
+    return 40960 + m * ((d + 511) // 512 * 1024 + 16) <= 163840
+
+
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("d", [5504, 11008, 18944, 28416, 56832])
-def test_matvec_of_long_rows_takes_tokens_in_batches(fmt, d):
-    """X does not fit a workgroup's LDS for all tokens, at the end for two: the same result, token by token."""
+@pytest.mark.parametrize("d", [3648, 5504, 11008, 18944, 28416, 60032])
+def test_matvec_of_long_rows_takes_windows_of_k(fmt, d):
+    """X does not fit a workgroup's LDS for all tokens, at the end for one: right, the same every time,
+    and the same token by token as long as the tokens fit."""
     import torch
     import paper_2607_26515_amd as P
     for n in (41, 1100 if d < 20000 else 70):  # fewer and more quads of rows than CUs
@@ -55,11 +61,39 @@ def test_matvec_of_long_rows_takes_tokens_in_batches(fmt, d):
         xb, wb, x, w = _case(fmt, 16, d, n, d + n)
         qc, qs = P.quantize(dev_bf16(wb), fmt, axis=1)
         tx = dev_bf16(xb)
-        y = P.matvec_w4a16(tx, qc, qs, fmt)
-        assert (np.abs(host(y) - x @ w.T) <= d * U * (np.abs(x) @ np.abs(w).T)).all()
-        for m in (1, 2, 3, 5, 7, 8, 9, 13):
-            assert torch.equal(P.matvec_w4a16(tx[:m], qc, qs, fmt), y[:m]), m
-        assert torch.equal(P.matvec_w4a16(tx[11:12], qc, qs, fmt, out="bf16"), y[11:12].bfloat16())
+        want, tol = x @ w.T, d * U * (np.abs(x) @ np.abs(w).T)
+        same = None
+        for m in (16, 13, 9, 8, 7, 5, 4, 3, 2, 1):
+            log(f"  m={m}")
+            y = P.matvec_w4a16(tx[:m], qc, qs, fmt)
+            assert (np.abs(host(y) - want[:m]) <= tol[:m]).all(), m
+            assert torch.equal(y, P.matvec_w4a16(tx[:m], qc, qs, fmt)), m
+            if _whole(m, d):
+                same = y if same is None else same
+                assert torch.equal(y, same[:m]), m
+            assert torch.equal(P.matvec_w4a16(tx[:m], qc, qs, fmt, out="bf16"), y.bfloat16()), m
+        # rows of X at odd addresses and strides, NaN between and behind them
+        for gap, shift in ((1, 0), (2, 1), (0, 3)):
+            buf = torch.full((16 * (d + gap) + shift + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            view = buf[shift:shift + 16 * (d + gap)].view(16, d + gap)[:, :d]
+            view.copy_(tx.view(torch.bfloat16))
+            assert torch.equal(P.matvec_w4a16(view, qc, qs, fmt), P.matvec_w4a16(tx, qc, qs, fmt)), (gap, shift)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_matvec_of_more_quads_than_wait_in_lds(fmt):
+    """More than 48 quads of rows to a workgroup, in windows of K, against the weights read out exactly."""
+    import torch
+    import paper_2607_26515_amd as P
+    m, d, n = 16, 4160, 50003
+    log(f"matvec {fmt} m={m} d={d} n={n}")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    qc, qs = P.quantize((torch.randn((n, d), generator=gen, device="cuda") * 0.02).bfloat16(), fmt)
+    x = torch.randn((m, d), generator=gen, device="cuda").bfloat16()
+    y = P.matvec_w4a16(x, qc, qs, fmt).double()
+    w = P.linear_w4a16(torch.eye(d, device="cuda").bfloat16(), qc, qs, fmt).double()  # Q(W)^T
+    want, mags = x.double() @ w, x.double().abs() @ w.abs()
+    assert ((y - want).abs() <= d * U * mags).all()
 
 
 @pytest.mark.parametrize("d", [9, 515, 1023, 8201, 12345, 16381])

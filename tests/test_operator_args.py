@@ -175,8 +175,8 @@ def test_refused_calls_keep_the_error_message_of_their_entry_point():
 
 def test_limits_of_lengths():
     """The longest row of the few-token product, the longest norm, and one step past each."""
-    assert matvec(d=56832, ldx=56832, X=0) == B.ERR_ARG  # gets as far as the operands
-    assert matvec(d=56832 + 64, ldx=56832 + 64) == B.ERR_UNSUPPORTED
+    assert matvec(d=(1 << 30) - 64, ldx=1 << 30, qw_codes=0) == B.ERR_ARG  # gets as far as the operands
+    assert matvec(d=1 << 30, ldx=1 << 30) == B.ERR_UNSUPPORTED
     assert fwd(d=16384, ldh=16384, ldy=16384, ldho=16384, ldx=16384, H=0) == B.ERR_ARG
     assert fwd(d=16385, ldh=16385, ldy=16385, ldho=16385, ldx=16385) == B.ERR_UNSUPPORTED
     assert lp(m=1 << 31) == B.ERR_UNSUPPORTED and lpb(m=1 << 31) == B.ERR_UNSUPPORTED
