@@ -570,6 +570,9 @@ def linear_fwd_swiglu(g, u, wprep, n, fmt, sparsity, y=None, ws=None, stream=Non
 # ------------------------------------------------------------------------------------------
 # operators around the linears
 # ------------------------------------------------------------------------------------------
+# They run on the current stream of their first tensor's device, or on `stream`, on which their outputs
+# and workspaces are then allocated; as everywhere in torch, inputs that another stream made or frees
+# are the caller's to order (wait_stream, record_stream).
 # (These helpers run on every call of operators whose kernels take a few microseconds: one pass over
 # each tensor's properties, torch looked up once.)
 _torch = None
