@@ -354,7 +354,8 @@ int resq_matvec_w4a16(int format, const uint16_t* X, int64_t m, int64_t d, int64
  *     X  = H' r_pre gamma_pre      of the rounded H'; bf16(f32(f32(H' r) gamma))
  * with r = 1 / sqrt(mean(row^2) + eps), the sum of squares in float64 and the rest as
  * resq_linear_fwd_prepared_rmsnorm defines it, so that X is the input that entry point forms.
- * H, H_out : m x d of h_dtype (RESQ_IN_BF16 or RESQ_IN_F32), row strides ldh, ldho.  H_out may be H.
+ * H, H_out : m x d of h_dtype (RESQ_IN_BF16 or RESQ_IN_F32), row strides ldh, ldho.  H_out may be H
+ *            (of the same stride, as wherever an output may be an input).
  * Y        : m x d of y_dtype, row stride ldy (a linear's output).  NULL: X = norm of H only; then
  *            gamma_pre is required, gamma_post and a gate are errors, and H_out is not written.
  * gamma_post, gamma_pre : d bf16 values, or NULL (no norm there; without gamma_pre X is not

@@ -291,6 +291,14 @@ int check_rows(const char* name, const void* p, int dtype, int64_t m, int64_t d,
   return RESQ_OK;
 }
 
+// An output in place of an input: row by row only.
+int check_in_place(const char* what, const void* in, int in_dtype, int64_t ld_in, const void* out, int out_dtype,
+                   int64_t ld_out, int64_t m) {
+  if (in != nullptr && in == out && (in_dtype != out_dtype || (m > 1 && ld_in != ld_out)))
+    return fail(RESQ_ERR_ARG, "%s in place need equal types and strides", what);
+  return RESQ_OK;
+}
+
 int check_gate(const void* gate, int gate_dtype, int gate_mode) {
   if (gate_mode != RESQ_GATE_NONE && gate_mode != RESQ_GATE_CHANNEL && gate_mode != RESQ_GATE_TOKEN)
     return fail(RESQ_ERR_ARG, "unknown gate mode %d", gate_mode);
@@ -832,6 +840,7 @@ int resq_block_norm_fwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_
   if (Y) {
     rc = check_rows("Y", Y, y_dtype, m, d, ldy);
     if (rc == RESQ_OK) rc = check_rows("H_out", H_out, h_dtype, m, d, ldho);
+    if (rc == RESQ_OK) rc = check_in_place("H and H_out", H, h_dtype, ldh, H_out, h_dtype, ldho, m);
     if (rc != RESQ_OK) return rc;
   } else if (gamma_post || gate_mode != RESQ_GATE_NONE || !gamma_pre) {
     return fail(RESQ_ERR_ARG, "without Y there is only the norm of H: gamma_pre, no gamma_post, no gate");
@@ -880,6 +889,7 @@ int resq_block_norm_bwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_
   if (rc == RESQ_OK && gamma_pre) rc = check_rows("dX", dX, dx_dtype, m, d, lddx);
   if (rc == RESQ_OK && dH_out) rc = check_rows("dH_out", dH_out, h_dtype, m, d, lddho);
   if (rc == RESQ_OK && dH) rc = check_rows("dH", dH, h_dtype, m, d, lddh);
+  if (rc == RESQ_OK) rc = check_in_place("dH_out and dH", dH_out, h_dtype, lddho, dH, h_dtype, lddh, m);
   if (rc == RESQ_OK && dY) rc = check_rows("dY", dY, dy_dtype, m, d, lddy);
   if (rc != RESQ_OK) return rc;
   const hipStream_t s = (hipStream_t)stream;
@@ -967,6 +977,7 @@ int resq_token_logprobs_bwd(const void* logits, int dtype, int64_t m, int64_t V,
                             int64_t ldd, void* stream) {
   int rc = check_logits(logits, dtype, m, V, ld, targets, temperature);
   if (rc == RESQ_OK) rc = check_rows("dlogits", dlogits, out_dtype, m, V, ldd);
+  if (rc == RESQ_OK) rc = check_in_place("logits and dlogits", logits, dtype, ld, dlogits, out_dtype, ldd, m);
   if (rc != RESQ_OK) return rc;
   if (m == 0) return ok();
   if (!targets || !stats) return fail(RESQ_ERR_ARG, "targets / stats is NULL");

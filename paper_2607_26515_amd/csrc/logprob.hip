@@ -183,7 +183,7 @@ __device__ __forceinline__ Sums wave_join(const Sums& a, float c, int lane) {
 }
 
 // Rows lie along y and z of a grid: a dimension holds less than 2^32 threads, and y and z 65535 workgroups.
-constexpr int64_t kGridRows = 32768;
+constexpr int64_t kGridRows = 65535;
 dim3 row_grid(int64_t x, int64_t rows) {
   return dim3((unsigned)x, (unsigned)std::min(rows, kGridRows), (unsigned)((rows + kGridRows - 1) / kGridRows));
 }

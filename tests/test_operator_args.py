@@ -181,3 +181,14 @@ def test_limits_of_lengths():
     assert fwd(d=16385, ldh=16385, ldy=16385, ldho=16385, ldx=16385) == B.ERR_UNSUPPORTED
     assert lp(m=1 << 31) == B.ERR_UNSUPPORTED and lpb(m=1 << 31) == B.ERR_UNSUPPORTED
     assert fwd(m=1 << 31) == B.ERR_UNSUPPORTED and bwd(m=1 << 31) == B.ERR_UNSUPPORTED
+
+
+def test_in_place_needs_equal_types_and_strides():
+    other = PTR + (1 << 12)
+    assert fwd(ldho=80, rstd=PTR + 2) == B.ERR_ARG and "rstd" not in P.resq_last_error()
+    assert bwd(lddh=80, workspace=0) == B.ERR_ARG
+    assert bwd(lddh=80, dH=other, workspace=0) == B.ERR_WORKSPACE  # gets as far as the workspace
+    assert bwd(m=1, lddh=80, workspace=0) == B.ERR_WORKSPACE       # one row has no stride
+    assert lpb(stats=0) == B.ERR_ARG and "in place" in P.resq_last_error()  # float32 logits, bf16 gradient
+    assert lpb(dtype=0, ldd=104, stats=0) == B.ERR_ARG and "in place" in P.resq_last_error()
+    assert lpb(dlogits=other, ldd=104, stats=0) == B.ERR_ARG and "in place" not in P.resq_last_error()
