@@ -299,11 +299,12 @@ int check_in_place(const char* what, const void* in, int in_dtype, int64_t ld_in
   return RESQ_OK;
 }
 
-int check_gate(const void* gate, int gate_dtype, int gate_mode) {
+int check_gate(const void* gate, int gate_dtype, int gate_mode, int64_t m, int64_t d) {
   if (gate_mode != RESQ_GATE_NONE && gate_mode != RESQ_GATE_CHANNEL && gate_mode != RESQ_GATE_TOKEN)
     return fail(RESQ_ERR_ARG, "unknown gate mode %d", gate_mode);
   if (gate_mode == RESQ_GATE_NONE) return RESQ_OK;
   if (!valid_dtype(gate_dtype)) return fail(RESQ_ERR_ARG, "unknown gate dtype %d", gate_dtype);
+  if ((gate_mode == RESQ_GATE_TOKEN ? m : d) == 0) return RESQ_OK;
   if (!gate || (uintptr_t)gate % (gate_dtype == RESQ_IN_F32 ? 4 : 2) != 0)
     return fail(RESQ_ERR_ARG, "gate must be non-NULL and aligned to its element");
   return RESQ_OK;
@@ -833,7 +834,7 @@ int resq_block_norm_fwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_
                         void* stream) {
   int rc = check_norm_sizes(m, d, alpha);
   if (rc == RESQ_OK) rc = check_rows("H", H, h_dtype, m, d, ldh);
-  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode);
+  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode, m, d);
   if (rc != RESQ_OK) return rc;
   if (!std::isfinite(eps) || !(eps >= 0x1p-126f))
     return fail(RESQ_ERR_ARG, "eps (%g) must be finite and at least 2^-126", (double)eps);
@@ -871,7 +872,7 @@ int resq_block_norm_bwd(const void* H, int h_dtype, int64_t m, int64_t d, int64_
                         float* dgamma_post, float* dgamma_pre, float* dgate, void* workspace,
                         size_t workspace_bytes, void* stream) {
   int rc = check_norm_sizes(m, d, alpha);
-  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode);
+  if (rc == RESQ_OK) rc = check_gate(gate, gate_dtype, gate_mode, m, d);
   if (rc != RESQ_OK) return rc;
   if (!valid_dtype(h_dtype)) return fail(RESQ_ERR_ARG, "unknown H dtype %d", h_dtype);
   if (!dH && !dY && !dgamma_post && !dgamma_pre && !dgate) return fail(RESQ_ERR_ARG, "no gradient is wanted");

@@ -17,6 +17,7 @@ function that needs it raises ``ResqError`` otherwise.  There is no fallback pat
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -333,7 +334,7 @@ def _sp(sp) -> int:
 
 
 def _p(t) -> int:
-    return 0 if t is None else int(t.data_ptr())
+    return 0 if t is None else t.data_ptr()
 
 
 def _stream(stream) -> int:
@@ -663,13 +664,19 @@ def _enter(index, stream):
     return ctx, _handle[0](index)
 
 
-def _ws_arg(lib, ws, op, m, d, n, dev):
+@functools.lru_cache(maxsize=256)
+def _ws_size(op, m, d, n) -> int:
+    return load().resq_workspace_size(op, 0, 0, m, d, n)
+
+
+def _ws_arg(ws, op, m, d, n, dev):
     """(tensor, address, bytes) of a workspace: the caller's, or one allocated on the current stream."""
     if ws is None:
-        nb = lib.resq_workspace_size(op, 0, 0, m, d, n)
+        nb = _ws_size(op, m, d, n)
         if nb == 0:
             return None, 0, 0
-        ws = _torch.empty(nb, dtype=_torch.uint8, device=dev), nb
+        buf = _torch.empty(nb, dtype=_torch.uint8, device=dev)
+        return buf, buf.data_ptr(), nb
     buf, nb = ws
     if buf.device != dev:
         raise ValueError(f"the workspace is on {buf.device}, not on {dev}")
@@ -758,20 +765,20 @@ def block_norm_bwd(h_out, rstd, dx=None, dh=None, y=None, gamma_post=None, gate=
     ctx, s = _enter(index, stream)
     try:
         f32, empty = torch.float32, torch.empty
-        r = {"dh": empty((m, d), dtype=_TYPES[hd], device=dev) if want_dh else None,
-             "dy": empty((m, d), dtype=_TYPES[yt], device=dev) if want_dy else None,
-             "dgamma_post": empty(d, dtype=f32, device=dev) if gamma_post is not None else None,
-             "dgamma_pre": empty(d, dtype=f32, device=dev) if gamma_pre is not None else None,
-             "dgate": None if gate is None else empty(gate.shape, dtype=f32, device=dev)}
-        keep, wp, nb = _ws_arg(lib, ws, OP_BLOCK_NORM_BWD, m, d, 0, dev)
+        gh = empty((m, d), dtype=_TYPES[hd], device=dev) if want_dh else None
+        gy = empty((m, d), dtype=_TYPES[yt], device=dev) if want_dy else None
+        gpo = empty(d, dtype=f32, device=dev) if gamma_post is not None else None
+        gpr = empty(d, dtype=f32, device=dev) if gamma_pre is not None else None
+        gg = empty(gate.shape, dtype=f32, device=dev) if gate is not None else None
+        keep, wp, nb = _ws_arg(ws, OP_BLOCK_NORM_BWD, m, d, 0, dev)
         rc = lib.resq_block_norm_bwd(h_out.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre,
-                                     rs, _p(dx), xd, lddx, _p(dh), lddho, _p(r["dh"]), d, _p(r["dy"]), yt, d,
-                                     _p(r["dgamma_post"]), _p(r["dgamma_pre"]), _p(r["dgate"]), wp, nb, s)
+                                     rs, _p(dx), xd, lddx, _p(dh), lddho, _p(gh), d, _p(gy), yt, d, _p(gpo),
+                                     _p(gpr), _p(gg), wp, nb, s)
     finally:
         if ctx is not None:
             ctx.__exit__(None, None, None)
     _check(rc, "resq_block_norm_bwd")
-    return r
+    return {"dh": gh, "dy": gy, "dgamma_post": gpo, "dgamma_pre": gpr, "dgate": gg}
 
 
 def matvec_w4a16(x, qw_codes, qw_scales, fmt, out="f32", y=None, stream=None):
@@ -831,7 +838,7 @@ def token_logprobs(logits, targets=None, temperature=1.0, top_k=0, ws=None, stre
             r["top_logp"] = empty((m, top_k), dtype=f32, device=dev)
             r["top_index"] = empty((m, top_k), dtype=torch.int32, device=dev)
             tv, ti = r["top_logp"].data_ptr(), r["top_index"].data_ptr()
-        keep, wp, nb = _ws_arg(lib, ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
+        keep, wp, nb = _ws_arg(ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
         rc = lib.resq_token_logprobs(logits.data_ptr(), dt, m, v, ld, tp, temperature, lp, r["stats"].data_ptr(), top_k,
                                      tv, ti, wp, nb, s)
     finally:

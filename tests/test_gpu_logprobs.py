@@ -40,7 +40,7 @@ def _close(got, want, tol, what):
     got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
     # outputs are float32: a value past (2 - 2^-24) 2^127, the midpoint between the largest float32 and
     # 2^128, rounds to infinity (a masked logit of the lowest value at a temperature below 1)
-    want = np.where(np.abs(want) >= (2 - 2.0 ** -24) * 2.0 ** 127, np.sign(want) * INF, want)
+    want = np.where(np.abs(want) >= (2 - 2.0 ** -24) * 2.0 ** 127, np.copysign(INF, want), want)
     same = (got == want) | (np.isnan(got) & np.isnan(want))
     with np.errstate(invalid="ignore"):
         bad = ~(same | (np.abs(got - want) <= tol + TINY) & np.isfinite(want))

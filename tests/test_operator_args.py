@@ -124,6 +124,7 @@ def test_empty_calls_succeed():
     assert fwd(m=0, H=0, Y=PTR, H_out=0, X=0) == B.OK
     assert matvec(m=0, X=0, Y=0) == B.OK and matvec(n=0, Y=0, ldy=0) == B.OK
     assert lp(m=0, logits=0) == B.OK and lpb(m=0, logits=0, dlogits=0) == B.OK
+    assert fwd(m=0, H=0, H_out=0, X=0, gate_mode=2, gate=0) == B.OK  # a gate of no rows
     assert P.resq_last_error() == ""
 
 
