@@ -382,6 +382,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
       }
     }
     if constexpr (kWide) {
+      if (k + 1 == trips) break;
       __builtin_amdgcn_sched_barrier(0);
       fetch(next);
       __builtin_amdgcn_sched_barrier(0);
