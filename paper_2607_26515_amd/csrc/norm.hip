@@ -254,7 +254,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
   };
   if constexpr (kWide)
     for (int i = 0; i < 2 * C * (E / 4); ++i) sums[i * 1024] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Raw<TH, E> raw_h[C], raw_e[C];
+  Raw<TH, E> raw_h[C], raw_e;
   Raw<TX, E> raw_x[C];
   Raw<TY, E> raw_y[C];
   Raw<uint16_t, E> raw_pre;
@@ -263,6 +263,9 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
     if (pre) load_raw(p.gamma_pre + col, raw_pre);
   };
   auto gain_branch = [&](uint32_t col) { branch_gain<E>(p.gamma_post, p.gate, p.gate_mode, p.gate_f32, p.alpha, col, w); };
+  auto fetch_e = [&](int64_t row, uint32_t col, Raw<TH, E>& to) {
+    if (p.dho) load_raw(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col, to);
+  };
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -271,18 +274,18 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
         load_raw(reinterpret_cast<const TH*>(p.h) + row * p.ldh + col, raw_h[c]);
         load_raw(reinterpret_cast<const TX*>(p.dx) + row * p.lddx + col, raw_x[c]);
       }
-      if (p.dho) load_raw(reinterpret_cast<const TH*>(p.dho) + row * p.lddho + col, raw_e[c]);
+      if constexpr (!kWide) fetch_e(row, col, raw_e);
       if (need_y) load_raw(reinterpret_cast<const TY*>(p.y) + row * p.ldy + col, raw_y[c]);
     }
   };
-  auto take = [&](int c, float rh, float ry, float hn[E], float dx[E], float e[E], float yn[E]) {
+  auto take = [&](int c, const Raw<TH, E>& raw_dh, float rh, float ry, float hn[E], float dx[E], float e[E], float yn[E]) {
     if (pre) {
       unpack(raw_h[c], hn);
       unpack(raw_x[c], dx);
 #pragma unroll
       for (int i = 0; i < E; ++i) hn[i] *= rh;
     }
-    if (p.dho) unpack(raw_e[c], e);
+    if (p.dho) unpack(raw_dh, e);
     else
 #pragma unroll
       for (int i = 0; i < E; ++i) e[i] = 0.f;
@@ -319,10 +322,14 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
         const Place<E> at = where(c);
         if constexpr (kWide) {
           __builtin_amdgcn_sched_barrier(0);
+          Raw<TH, E> raw_dh;
+          fetch_e(row, at.col, raw_dh);
           gain_pre(at.col);
           gain_branch(at.col);
+          take(c, raw_dh, rh, ry, hn[c], dx, e[c], yn[c]);
+        } else {
+          take(c, raw_e, rh, ry, hn[c], dx, e[c], yn[c]);
         }
-        take(c, rh, ry, hn[c], dx, e[c], yn[c]);
         if constexpr (!kWide) fetch(next);
         if (pre) {
           float g[E], x[E];
