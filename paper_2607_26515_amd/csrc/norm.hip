@@ -233,9 +233,11 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(NormBwd p, int L) {
     if constexpr (C > 1) asm("" : "+v"(l));
     return place<E>(c, L, l, d);
   };
-  // Column sums: in registers for one group per lane, in LDS for more (each lane adds to its own).  With
-  // them in registers too, rows longer than 8192 had to be read a second time after the row sums: 1792 x
-  // 16384 took 194 us (bf16 h) and 256 us (float32) instead of 153 and 229.
+  // Column sums: in registers for one group per lane, in LDS for more (each lane adds to its own): with them in
+  // registers too, rows longer than 8192 had to be read a second time after the row sums (1792 x 16384: 194 us
+  // with bf16 streams and 256 in float32, now 144 and 192).  Such a row's operands fill a CU's registers: the
+  // next row's h, y and dx are loaded behind this row's stores, dh' and the gains group by group, and what is
+  // loaded under a condition is declared inside the loop (outside, the last row's would be kept).
   constexpr bool kWide = C > 1;
   extern __shared__ __attribute__((aligned(16))) uint8_t column_lds[];
   f32x4* sums = reinterpret_cast<f32x4*>(column_lds) + threadIdx.x;  // [pre, branch][C][E / 4][1024]
