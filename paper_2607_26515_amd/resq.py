@@ -718,7 +718,7 @@ def block_norm(h, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None,
         if y is None:
             h_out, ldho = h, ldh
         elif h_out is None:
-            h_out, ldho = torch.empty((m, d), dtype=h.dtype, device=h.device), d
+            h_out, ldho = torch.empty(m, d, dtype=h.dtype, device=h.device), d
         else:
             if h_out.dtype != h.dtype:
                 raise TypeError(f"h_out has type {h_out.dtype}, h {h.dtype}")
@@ -727,12 +727,12 @@ def block_norm(h, y=None, gamma_post=None, gate=None, alpha=1.0, gamma_pre=None,
         if gamma_pre is None:
             x = None
         elif x is None:
-            x = torch.empty((m, d), dtype=torch.bfloat16, device=h.device)
+            x = torch.empty(m, d, dtype=torch.bfloat16, device=h.device)
         else:
             if _dtype(x, "x") != IN_BF16:
                 raise TypeError("x must be bfloat16")
             ldx = _rows(x, "x", m, d, index)
-        rstd = torch.empty((2, m), dtype=torch.float32, device=h.device) if save else None
+        rstd = torch.empty(2, m, dtype=torch.float32, device=h.device) if save else None
         rc = lib.resq_block_norm_fwd(h.data_ptr(), hd, m, d, ldh, _p(y), yd, ldy, gpost, g, gd, gm, alpha, gpre, eps,
                                      h_out.data_ptr(), ldho, _p(x), ldx, _p(rstd), s)
     finally:
@@ -765,8 +765,8 @@ def block_norm_bwd(h_out, rstd, dx=None, dh=None, y=None, gamma_post=None, gate=
     ctx, s = _enter(index, stream)
     try:
         f32, empty = torch.float32, torch.empty
-        gh = empty((m, d), dtype=_TYPES[hd], device=dev) if want_dh else None
-        gy = empty((m, d), dtype=_TYPES[yt], device=dev) if want_dy else None
+        gh = empty(m, d, dtype=_TYPES[hd], device=dev) if want_dh else None
+        gy = empty(m, d, dtype=_TYPES[yt], device=dev) if want_dy else None
         gpo = empty(d, dtype=f32, device=dev) if gamma_post is not None else None
         gpr = empty(d, dtype=f32, device=dev) if gamma_pre is not None else None
         gg = empty(gate.shape, dtype=f32, device=dev) if gate is not None else None
@@ -802,7 +802,7 @@ def matvec_w4a16(x, qw_codes, qw_scales, fmt, out="f32", y=None, stream=None):
     ctx, s = _enter(index, stream)
     try:
         if y is None:
-            y, ldy = torch.empty((m, n), dtype=_TYPES[yt], device=x.device), n
+            y, ldy = torch.empty(m, n, dtype=_TYPES[yt], device=x.device), n
         else:
             if _dtype(y, "y") != yt:
                 raise TypeError(f"y has type {y.dtype}, out is {out!r}")
@@ -833,10 +833,10 @@ def token_logprobs(logits, targets=None, temperature=1.0, top_k=0, ws=None, stre
         if targets is not None:
             r["logp"] = empty(m, dtype=f32, device=dev)
             lp = r["logp"].data_ptr()
-        r["stats"] = empty((m, 3), dtype=f32, device=dev)
+        r["stats"] = empty(m, 3, dtype=f32, device=dev)
         if top_k > 0:
-            r["top_logp"] = empty((m, top_k), dtype=f32, device=dev)
-            r["top_index"] = empty((m, top_k), dtype=torch.int32, device=dev)
+            r["top_logp"] = empty(m, top_k, dtype=f32, device=dev)
+            r["top_index"] = empty(m, top_k, dtype=torch.int32, device=dev)
             tv, ti = r["top_logp"].data_ptr(), r["top_index"].data_ptr()
         keep, wp, nb = _ws_arg(ws, OP_TOKEN_LOGPROBS, m, v, max(top_k, 0), dev)
         rc = lib.resq_token_logprobs(logits.data_ptr(), dt, m, v, ld, tp, temperature, lp, r["stats"].data_ptr(), top_k,
@@ -862,7 +862,7 @@ def token_logprobs_bwd(logits, targets, stats, dlogp=None, dentropy=None, temper
     ctx, s = _enter(index, stream)
     try:
         if dlogits is None:
-            dlogits, ldd = torch.empty((m, v), dtype=_TYPES[ot], device=logits.device), v
+            dlogits, ldd = torch.empty(m, v, dtype=_TYPES[ot], device=logits.device), v
         else:
             if _dtype(dlogits, "dlogits") != ot:
                 raise TypeError(f"dlogits has type {dlogits.dtype}, out is {out!r}")
