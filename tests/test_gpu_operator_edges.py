@@ -172,3 +172,19 @@ def test_profiler_families():
             assert got[0] == calls and 0 < got[1] < 1000, (name, got)
     finally:
         P.resq_profile_enable(0)
+
+
+def test_readme_examples_run_one_after_the_other():
+    import os
+    import re
+    import torch
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    env = {}
+    for block in re.findall(r"```python\n(.*?)```", text, re.S):
+        exec(compile(block, "README.md", "exec"), env)  # noqa: S102 - the repository's own README
+    torch.cuda.synchronize()
+    assert env["h"].shape == env["x"].shape == (4, 2048) and env["q"].shape == (4, 2560)
+    assert env["t"]["logp"].shape == (4,) and env["t"]["logp"][2] == 0 and env["t"]["top_index"].shape == (4, 5)
+    assert env["dq"].shape == (4, 2560) and (env["dq"][2] == 0).all()
+    assert env["g"]["dh"].shape == env["g"]["dy"].shape == (4, 2048) and env["g"]["dgamma_pre"].shape == (2048,)
+    assert bool(torch.isfinite(env["g"]["dgamma_pre"]).all()) and bool(torch.isfinite(env["t"]["top_logp"][[0, 1, 3]]).all())
