@@ -24,7 +24,7 @@
 //
 // Measured (a large copy runs at 5.08 TB/s): 2047 x 100003 bf16 64 us, 5.1 TB/s; 1024 x 131072 float32
 // 99 us, 5.4 TB/s; 256 x 131072 float32 with 5 alternatives 33 us, the join of its four splits 4 of them;
-// 1881 x 22901 bf16 25 us, with 20 alternatives 38; one row of 131072 with 20 alternatives 6.5 + 5.2 us, two
+// 1881 x 22901 bf16 25 us, with 20 alternatives 38; one row of 131072 with 20 alternatives 10.7 us, two
 // launches' latency.  Gradient: 1024 x 131072 float32 to bf16 128 us, 5.5 TB/s.
 #include <algorithm>
 
@@ -437,10 +437,16 @@ __global__ __launch_bounds__(64 * kJoinWaves) void logprob_join_kernel(Args a) {
   finish<T>(a, row, s, list, lane);
 }
 
-// Workgroups per row: enough to give every CU four, none with less than a load per lane.
-int64_t splits_of(int64_t m, int64_t V) {
+// Workgroups per row: enough to give every CU four, but with alternatives none with less than kUnroll loads
+// per lane (1 x 131072, top 20: 11.2 us with one load, 10.7; top 32 of 8 x 151111: 13.5, 12.4), and one where
+// kWhole loads do: that saves the second launch (148 x 20942: 9.2 us in six, 7.8 in one, with top 5 14.4 and
+// 10.1; 35 x 50742: 7.5 in parts, 8.3 in one, with top 5 12.2 and 10.8).
+constexpr int64_t kWhole = 12;
+int64_t splits_of(int64_t m, int64_t V, bool top) {
   const int64_t step = 64 * kGroup * waves_for(V), want = std::max<int64_t>(1, 1024 / std::max<int64_t>(m, 1));
-  const int64_t trips = (V + step - 1) / step, per = (trips + want - 1) / want;
+  const int64_t trips = (V + step - 1) / step;
+  if (trips <= kWhole) return 1;
+  const int64_t per = std::max<int64_t>((trips + want - 1) / want, top ? kUnroll : 1);
   return (trips + per - 1) / per;
 }
 int64_t split_len(int64_t V, int64_t splits) {
@@ -490,7 +496,7 @@ __global__ __launch_bounds__(kBwdThreads) void logprob_bwd_kernel(LogprobBwd p, 
 
 size_t logprob_ws_bytes(int64_t m, int64_t V, int top_k) {
   if (m <= 0 || V <= 0) return 0;
-  const int64_t sp = splits_of(m, V);
+  const int64_t sp = splits_of(m, V, top_k > 0);
   if (sp == 1) return 0;
   return up256((size_t)(m * sp) * sizeof(Sums)) + (top_k > 0 ? (size_t)(m * sp) * 32 * 8 : 0);
 }
@@ -500,7 +506,7 @@ void launch_logprob_fwd(const LogprobFwd& p, bool f32, void* workspace, hipStrea
   a.p = p;
   a.c = (float)(1.4426950408889634 / p.temperature);
   a.inv_t = (float)(1.0 / p.temperature);
-  a.splits = splits_of(p.m, p.V);
+  a.splits = splits_of(p.m, p.V, p.top_k > 0);
   a.len = split_len(p.V, a.splits);
   a.sums = (Sums*)workspace;
   a.keys = (uint64_t*)((char*)workspace + up256((size_t)(p.m * a.splits) * sizeof(Sums)));
